@@ -350,6 +350,120 @@ tdk_status tdk_restore_layers(tdk_round* r, int32_t first_layer, int32_t n_layer
                               const tdk_layer_io* io, const tdk_diff* diffs, const tdk_pingpong* pp,
                               void* compute_stream, void* copy_stream);
 
+/* ---- The agents' own tokens -----------------------------------------------------------------------------
+ * What a model does with the paged caches between two rounds: the tokens it has just computed are appended
+ * (tdk_kv_append), their queries attend to the cache (tdk_kv_attend), and finished outputs leave it again as
+ * the masters of the next round (tdk_kv_read).  One call covers a batch of sequences of any lengths; all of a
+ * batch's description lies on the device, so a captured call serves every later step of the same sizes.
+ *
+ * A cache has one of two formats:
+ *   TDK_KV_BF16    planes [pool_pages][T][H][D] bf16: the pool of the rounds (tdk_layer_io.pool_k / pool_v)
+ *   TDK_KV_MXFP4   planes [pool_pages][H][T * 64 + T * 4] bytes, 3.8 times smaller: per page and KV head the 4-bit
+ *                  values of its T tokens (64 bytes each, element 2 i in the low half of byte i), then the
+ *                  block exponents (4 bytes each).  A value is one sign, two exponent bits and one mantissa bit
+ *                  (magnitudes 0 0.5 1 1.5 2 3 4 6); 32 consecutive elements of a row share a power of two
+ *                  2^(byte - 127); byte 255 makes all 32 NaN. */
+#define TDK_KV_BF16  0
+#define TDK_KV_MXFP4 1
+
+typedef struct tdk_kv tdk_kv;   /* opaque, host memory only: geometry, format, rotation frequencies, device */
+
+/* num_layers of the model is not used.  A handle belongs to the device that is current when it is created; calls
+ * with another device current fail with INVALID_ARG.  It holds no state between calls: calls may run at the
+ * same time on several streams and from several threads.  Errors: INVALID_ARG, UNSUPPORTED (as
+ * tdk_round_create; unknown format), NOMEM. */
+tdk_status tdk_kv_create(const tdk_model* model, int32_t format, tdk_kv** out);
+void       tdk_kv_destroy(tdk_kv* kv);               /* NULL-safe; work that is enqueued already is not affected */
+size_t     tdk_kv_page_bytes(const tdk_kv* kv);      /* bytes of one page in one plane; 0 for NULL */
+
+/* One layer of a cache, DEV, 16-byte aligned. */
+typedef struct {
+  void*   k;
+  void*   v;
+  int64_t pool_pages;
+} tdk_kv_cache;
+
+/* A batch of sequences.  Sequence s has seq_len[s] tokens in all, and the last n_s = q_start[s + 1] - q_start[s]
+ * of them are the batch's: its token t (position seq_len[s] - n_s + t) is row q_start[s] + t of the token buffers.
+ *   n_tokens   rows of the token buffers; q_start[n_seqs] may be smaller: the rows behind it are left alone
+ *   max_len    longest sequence that is expected: how a call is cut into workgroups goes by it and by the
+ *              sizes above, results do not (a longer sequence is served too, only more slowly)
+ * Token j lies in physical page block_table[s][j / T].  q_start must not decrease.  Everything on the device is
+ * checked there: starts are cut to [0, n_tokens], and a token whose position is negative, whose logical page
+ * lies past table_stride or whose page number is not in [0, pool_pages) is not written by append, reads as zero
+ * and is seen by no query.  At most 2^30 tokens per call, and per sequence by its table (else UNSUPPORTED). */
+typedef struct {
+  int32_t        n_seqs;
+  int32_t        n_tokens;
+  int32_t        max_len;
+  const int32_t* q_start;       /* DEV [n_seqs + 1] */
+  const int32_t* seq_len;       /* DEV [n_seqs]     */
+  const int32_t* block_table;   /* DEV [n_seqs][table_stride] */
+  int32_t        table_stride;
+} tdk_kv_batch;
+
+/* Rows of tokens, DEV, bf16, 16-byte aligned.  Row r of k starts at element r * k_stride and holds [H][D]; strides
+ * are multiples of 8, at least H * D (n_q_heads * D), so that k, v and q may be slices of one projection's output. */
+typedef struct {
+  void*       k;
+  void*       v;
+  int64_t     k_stride;
+  int64_t     v_stride;
+  const void* q;                /* tdk_kv_append only: queries to rotate as well, or NULL */
+  int64_t     q_stride;
+  int32_t     n_q_heads;
+  void*       q_out;            /* may be q itself, with the same stride */
+  int64_t     q_out_stride;
+} tdk_kv_rows;
+
+/* Writes the batch's tokens into the cache: K (un-rotated in `rows`) rotated for each token's position in the
+ * arithmetic above, V as it is; with q, the rotated queries into q_out.  MXFP4: the fp32 values go to the nearest
+ * 4-bit value of their block (ties to even); the block's power of two is 2^(floor(log2 m) - 2) of its largest
+ * magnitude m, one higher from m = 1.75 * 2^n on (what lies beyond 6 becomes 6); a block with an infinity or NaN
+ * becomes NaN.  Tokens must lie in pages that no other token of the batch is written to.  One kernel. */
+tdk_status tdk_kv_append(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
+                         const tdk_kv_rows* rows, void* hip_stream);
+
+/* The inverse: the batch's tokens out of the cache into rows->k / rows->v (the same rows that append would take;
+ * K stays rotated; 4-bit values are exact in bf16).  rows->q must be NULL.  One kernel. */
+tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
+                       const tdk_kv_rows* rows, void* hip_stream);
+
+/* Attention of the batch's tokens to their sequences.  The query at position p of sequence s sees token j iff
+ *   j <= p,  and  window = 0 or j > p - window or j < n_sink,  and not hole[s][0] <= j < hole[s][1].
+ *   q          bf16 rows [n_q_heads][D], rotated; query head hq reads KV head hq / (n_q_heads / H)
+ *   out        bf16 rows [n_q_heads][D]: softmax(scale * q . K) V over what the query sees; zero if it sees nothing
+ *   lse        fp32 [n_tokens][n_q_heads]: log of the softmax denominator, -inf for a query that sees nothing; may be NULL
+ *   hole       DEV int32 [n_seqs][2], or NULL: tokens attended to elsewhere (the shared span, tdk_attend_shared)
+ *   part_out, part_lse   DEV fp32 [n_tokens][n_q_heads][D] and [n_tokens][n_q_heads], or NULL: a partial result over other
+ *              tokens, as tdk_attend_shared leaves it; out and lse are then those of both parts together
+ *   workspace  tdk_kv_attend_workspace_bytes() bytes, 256-byte aligned, contents undefined; calls that may run at the same
+ *              time (two streams, two graphs) need one each
+ * Any finite scale is taken.  What a query does not see does not reach its result, whatever it holds (NaN and
+ * infinities included).  bf16 products with fp32 sums; the softmax weights are rounded to bf16 for the second product,
+ * their sum is not.  Allocates nothing, one or two kernels, does not synchronise; results do not depend on what else runs. */
+typedef struct {
+  const void*    q;
+  int64_t        q_stride;      /* elements, a multiple of 8, at least n_q_heads * D */
+  int32_t        n_q_heads;
+  float          scale;
+  void*          out;
+  int64_t        out_stride;
+  float*         lse;
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t        window;        /* 0: none */
+  int32_t        n_sink;        /* first tokens that stay visible behind a window */
+  const int32_t* hole;
+  const float*   part_out;
+  const float*   part_lse;
+} tdk_kv_attend_io;
+
+/* Depends on n_seqs, n_tokens and max_len only (nothing on the device is read); 0 where none is needed or on bad arguments. */
+size_t     tdk_kv_attend_workspace_bytes(const tdk_kv* kv, const tdk_kv_batch* batch, int32_t n_q_heads);
+tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
+                         const tdk_kv_attend_io* a, void* hip_stream);
+
 /* Storage arithmetic of Sec. 6.4 (host only). */
 double tdk_dense_bytes(const tdk_model* m, int64_t span_tokens);   /* one layer of one cache      */
 double tdk_diff_bytes(const tdk_model* m, int64_t diff_pages);     /* values + idx + count/offset */

@@ -12,6 +12,7 @@
 
 #include "tdk_internal.h"
 #include "tdk_bench.h"
+#include "tdk_errors.h"
 #include "tdk_plan.h"
 
 using namespace tdk;
@@ -23,36 +24,11 @@ static __device__ __align__(256) unsigned char scratch[TDK_STATIC_SCRATCH_BYTES]
 
 namespace {
 
-thread_local std::string g_last_error;
-
 constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mutex;
 void* g_scratch_ptr[kMaxDevices] = {nullptr};     // device address of `scratch` on each device, once resolved
 
-tdk_status fail(tdk_status st, const std::string& msg) {
-  g_last_error = msg;
-  return st;
-}
-
-tdk_status hip_fail(hipError_t e, const char* what) {
-  return fail(TDK_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// No exception leaves the library: host allocations that fail become TDK_ERR_NOMEM.
-template <typename F>
-tdk_status guarded(F&& body) {
-  try {
-    return body();
-  } catch (const std::bad_alloc&) {
-    try { g_last_error = "out of memory"; } catch (...) {}   // short enough to need no allocation
-    return TDK_ERR_NOMEM;
-  } catch (...) {
-    try { g_last_error = "internal error"; } catch (...) {}
-    return TDK_ERR_INVALID_ARG;
-  }
-}
 
 using HostSession = tdk::PlanSession;
 

@@ -1,0 +1,695 @@
+// Caches that programs append to: new tokens into the pages (rotated on the way, in bf16 or in 4 bits), attention of their
+// queries to the pages, and rows back out of them.
+#include "tdk_kv.h"
+
+#include <algorithm>
+
+namespace tdk {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+namespace {
+
+constexpr int kRow = 2 * kHeadDim;         // bytes of a bf16 head row
+constexpr int kRow4 = kHeadDim / 2;        // bytes of its 4-bit values
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Orders the LDS traffic of one wavefront: no hardware barrier, only a point the compiler may not move memory accesses across.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// For i in [0, n), at(i) not decreasing: how many are <= x.  The lanes of a wavefront probe 64 places a round (one round up to
+// 64 entries, two up to 4096).  A round leaves less than a 64th of the range, whatever the values are.
+template <class F>
+__device__ __forceinline__ int count_up_to(F at, int n, int64_t x, int lane) {
+  int lo = 0, hi = n;
+  while (hi > lo) {
+    const int step = (hi - lo + 63) / 64;
+    const int64_t i = lo + (int64_t)step * (lane + 1) - 1;
+    const bool le = i < hi && at((int)i) <= x;
+    const int c = __popcll(__ballot(le));
+    const int64_t next = lo + (int64_t)step * c, last = lo + (int64_t)step * (c + 1) - 1;
+    lo = (int)min((int64_t)hi, next);
+    hi = (int)max((int64_t)lo, min((int64_t)hi, last));
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// A start out of q_start, cut to the token buffers.
+__device__ __forceinline__ int start_of(const KvDev& kv, int i) { return min(max(kv.q_start[i], 0), kv.n_tokens); }
+
+// Physical page of a sequence's logical page, -1 where there is none.
+__device__ __forceinline__ int page_of(const KvDev& kv, int s, int64_t lp) {
+  if (lp < 0 || lp >= kv.table_stride) return -1;
+  const int p = kv.table[(int64_t)s * kv.table_stride + lp];
+  return p >= 0 && p < kv.pool_pages ? p : -1;
+}
+
+// Where a row of the token buffers belongs: -1 for rows that no sequence has or whose place the table does not name.
+struct Slot { int page, at, pos; };
+__device__ __forceinline__ Slot slot_of(const KvDev& kv, int row, int lane) {
+  const int s = count_up_to([&](int i) { return (int64_t)start_of(kv, i + 1); }, kv.n_seqs, row, lane);
+  Slot o{-1, 0, -1};
+  if (s >= kv.n_seqs) return o;
+  const int q0 = start_of(kv, s), q1 = start_of(kv, s + 1);
+  if (row < q0 || row >= q1) return o;
+  const int pos = max(kv.seq_len[s], 0) - (q1 - row);
+  if (pos < 0) return o;
+  o.page = page_of(kv, s, pos >> kv.page_shift);
+  o.at = pos & ((1 << kv.page_shift) - 1);
+  o.pos = pos;
+  return o;
+}
+
+// The four block exponents and the places of a head row in a 4-bit page.
+__device__ __forceinline__ char* row4(char* plane, const KvDev& kv, const Slot& o, int h) {
+  const int T = 1 << kv.page_shift;
+  return plane + ((int64_t)o.page * kv.heads + h) * (T * 68) + o.at * kRow4;
+}
+__device__ __forceinline__ char* scale4(char* plane, const KvDev& kv, const Slot& o, int h) {
+  const int T = 1 << kv.page_shift;
+  return plane + ((int64_t)o.page * kv.heads + h) * (T * 68) + T * kRow4 + o.at * 4;
+}
+
+__device__ __forceinline__ uint32_t top_bits(const float (&x)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  // the block: four lanes of eight elements
+  m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+  return max(m, (uint32_t)__shfl_xor((int)m, 2));
+}
+
+// The byte of a block's power of two from the bits of its largest magnitude: the exponent, one more where the mantissa is 1.75 or
+// above (a carry out of the bits below), less the two of the largest 4-bit value.  Infinities and NaN lie above all numbers.
+__device__ __forceinline__ uint32_t block_exponent(uint32_t top) {
+  if (top >= 0x7f800000u) return 255;
+  const int e = (int)((top + 0x200000u) >> 23) - 2;
+  return (uint32_t)max(e, 1);
+}
+
+__device__ __forceinline__ uint32_t to4(const float (&x)[8], uint32_t e) {
+  if (e == 255) return 0;
+  const float unit = __uint_as_float(e << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
+  return w;
+}
+
+// Eight 4-bit values times their block's power of two, exact in bf16 (a byte of 255 gives NaN).
+__device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
+  const float unit = __uint_as_float(e << 23);
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3))};
+}
+
+// ---------------------------------------------------------------------------------------------
+// Append: a token's K and Q heads rotated, its V heads as they are.  Lane (hl, c) = (lane / 8, lane % 8) holds elements 8 c .. + 7 and
+// 64 + 8 c .. + 7 of head 8 step + hl of the list K heads, Q heads, V heads: both halves of every pair of either style.
+// Every lane evaluates one of the 64 angles in double and passes cosine and sine (rounded to fp32 once) on through LDS.
+// ---------------------------------------------------------------------------------------------
+template <bool FOUR>
+__global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const KvRowsDev rows) {
+  __shared__ float2 turn[kHalf];
+  const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
+  const int row = blockIdx.x / rows.waves, part = blockIdx.x - row * rows.waves;
+  const Slot o = slot_of(kv, row, lane);
+  if (o.pos < 0) return;                             // (the queries of a token with no page are rotated all the same)
+  double sn, cs;
+  sincos((double)o.pos * rows.inv_freq[lane], &sn, &cs);
+  turn[lane] = make_float2((float)cs, (float)sn);
+  wave_sync();
+  float2 t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = turn[kv.interleaved ? 4 * c + (i & 3) + 32 * (i >> 2) : 8 * c + i];
+  const int H = kv.heads, HQ = rows.n_q_heads, n = 2 * H + HQ;
+  for (int step = part; 8 * step < n; step += rows.waves) {
+    const int e = 8 * step + hl;
+    const bool is_k = e < H, is_q = !is_k && e < H + HQ, on = e < n;
+    const int h = is_k ? e : is_q ? e - H : e - H - HQ;
+    u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    if (on) {
+      const char* src = is_k ? rows.k + row * rows.k_stride : is_q ? rows.q + row * rows.q_stride : rows.v + row * rows.v_stride;
+      a = *reinterpret_cast<const u32x4*>(src + h * kRow + 16 * c);
+      b = *reinterpret_cast<const u32x4*>(src + h * kRow + 16 * c + 128);
+    }
+    float x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = lo16(a[i]); x[2 * i + 1] = hi16(a[i]);
+      y[2 * i] = lo16(b[i]); y[2 * i + 1] = hi16(b[i]);
+    }
+    if (is_k || is_q) {
+      if (kv.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float xa = x[2 * i], xb = x[2 * i + 1], ya = y[2 * i], yb = y[2 * i + 1];
+          x[2 * i] = __builtin_fmaf(xa, t[i].x, -(xb * t[i].y));
+          x[2 * i + 1] = __builtin_fmaf(xb, t[i].x, xa * t[i].y);
+          y[2 * i] = __builtin_fmaf(ya, t[4 + i].x, -(yb * t[4 + i].y));
+          y[2 * i + 1] = __builtin_fmaf(yb, t[4 + i].x, ya * t[4 + i].y);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float xa = x[i], xb = y[i];
+          x[i] = __builtin_fmaf(xa, t[i].x, -(xb * t[i].y));
+          y[i] = __builtin_fmaf(xb, t[i].x, xa * t[i].y);
+        }
+      }
+    }
+    if (!FOUR || is_q) {
+      if (!on || (!is_q && o.page < 0)) continue;
+      char* dst = is_q ? rows.q_out + row * rows.q_out_stride + h * kRow
+                       : (is_k ? kv.k : kv.v) + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = pack2(x[2 * i], x[2 * i + 1]);
+        b[i] = pack2(y[2 * i], y[2 * i + 1]);
+      }
+      if (!is_k && !is_q) {                          // values move as they are, NaN payloads included
+        const char* src = rows.v + row * rows.v_stride + h * kRow + 16 * c;
+        a = *reinterpret_cast<const u32x4*>(src);
+        b = *reinterpret_cast<const u32x4*>(src + 128);
+      }
+      *reinterpret_cast<u32x4*>(dst + 16 * c) = a;
+      *reinterpret_cast<u32x4*>(dst + 16 * c + 128) = b;
+    } else {
+      // (lanes of one block always take the same way here: they hold the same head)
+      const uint32_t ex = block_exponent(top_bits(x)), ey = block_exponent(top_bits(y));
+      const uint32_t wx = to4(x, ex), wy = to4(y, ey);
+      const uint32_t ex1 = (uint32_t)__shfl_xor((int)ex, 4), ey1 = (uint32_t)__shfl_xor((int)ey, 4);
+      if (!on || o.page < 0) continue;
+      char* dst = row4(is_k ? kv.k : kv.v, kv, o, h);
+      *reinterpret_cast<uint32_t*>(dst + 4 * c) = wx;
+      *reinterpret_cast<uint32_t*>(dst + 32 + 4 * c) = wy;
+      if (c == 0) *reinterpret_cast<uint32_t*>(scale4(is_k ? kv.k : kv.v, kv, o, h)) = ex | ex1 << 8 | ey << 16 | ey1 << 24;
+    }
+  }
+}
+
+// Read: the same lanes, from the cache to rows.
+template <bool FOUR>
+__global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const KvRowsDev rows) {
+  const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
+  const int row = blockIdx.x / rows.waves, part = blockIdx.x - row * rows.waves;
+  const int s = count_up_to([&](int i) { return (int64_t)start_of(kv, i + 1); }, kv.n_seqs, row, lane);
+  if (s >= kv.n_seqs || row < start_of(kv, s)) return;      // rows of no sequence stay as they are
+  const Slot o = slot_of(kv, row, lane);
+  const int H = kv.heads;
+  for (int step = part; 8 * step < 2 * H; step += rows.waves) {
+    const int e = 8 * step + hl;
+    if (e >= 2 * H) continue;
+    const bool is_k = e < H;
+    const int h = is_k ? e : e - H;
+    u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    if (o.page >= 0) {
+      char* plane = is_k ? kv.k : kv.v;
+      if (FOUR) {
+        const char* src = row4(plane, kv, o, h);
+        const uint32_t ex = *reinterpret_cast<const uint32_t*>(scale4(plane, kv, o, h));
+        a = from4(*reinterpret_cast<const uint32_t*>(src + 4 * c), ex >> (8 * (c >> 2)) & 255u);
+        b = from4(*reinterpret_cast<const uint32_t*>(src + 32 + 4 * c), ex >> (8 * (c >> 2) + 16) & 255u);
+      } else {
+        const char* src = plane + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow + 16 * c;
+        a = *reinterpret_cast<const u32x4*>(src);
+        b = *reinterpret_cast<const u32x4*>(src + 128);
+      }
+    }
+    char* dst = (is_k ? rows.k + row * rows.k_stride : rows.v + row * rows.v_stride) + h * kRow + 16 * c;
+    *reinterpret_cast<u32x4*>(dst) = a;
+    *reinterpret_cast<u32x4*>(dst + 128) = b;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention.  The query rows of a sequence and KV head are its (token, head of the group) pairs, tokens first; a workgroup takes a
+// block of them and a part of the tokens they see.  Scores are kept in base 2: s = (q . k) scale log2(e).
+// ---------------------------------------------------------------------------------------------
+constexpr int kTile = 32;                  // tokens per step of a wavefront
+constexpr int kVsStride = kHeadDim + 32;   // bf16 elements per staged V row (+64 bytes: four rows' 64-byte pieces then lie in different
+                                           // LDS banks for the transposing reads)
+
+// A block of query rows: which sequence it belongs to, and what its rows see.
+struct Block {
+  int s;              // sequence
+  int q0;             // first row of the token buffers
+  int n_rows;         // query rows of the sequence
+  int r0;             // first row of the block
+  int pos0;           // position of the sequence's first new token (may be negative)
+  int p_lo, p_hi;     // positions of the block's first and last row
+  int hole_b, hole_e;
+};
+
+// Row blocks are numbered without knowing the lengths: sequence s starts at number floor(q0 group / block) + s, which leaves at least
+// as many numbers as it has blocks.  False: no block has this number.
+__device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& at, int id, int block_rows, int lane, Block& b) {
+  const auto first = [&](int i) { return (int64_t)start_of(kv, i) * at.group / block_rows + i; };
+  b.s = count_up_to(first, kv.n_seqs, id, lane) - 1;
+  if (b.s < 0) return false;
+  b.q0 = start_of(kv, b.s);
+  const int n = start_of(kv, b.s + 1) - b.q0;
+  if (n <= 0) return false;
+  b.n_rows = n * at.group;                   // (at most n_tokens * n_q_heads, which the host has checked)
+  const int64_t r0 = (id - first(b.s)) * block_rows;
+  if (r0 >= b.n_rows) return false;
+  b.r0 = (int)r0;
+  b.pos0 = max(kv.seq_len[b.s], 0) - n;      // (tokens of a call and of a table are at most 2^30: differences of positions fit)
+  b.p_lo = b.pos0 + b.r0 / at.group;
+  b.p_hi = b.pos0 + (min(b.r0 + block_rows, b.n_rows) - 1) / at.group;
+  b.hole_b = at.hole ? at.hole[2 * b.s] : 0;
+  b.hole_e = at.hole ? max(at.hole[2 * b.s + 1], b.hole_b) : 0;
+  return true;
+}
+
+// The tiles that hold what some row of the block sees: at most four runs in ascending order (first tokens and window, each before and
+// behind the hole).
+struct Tiles {
+  int begin[4], count[4], total;
+  __device__ __forceinline__ int tile(int i) const {
+    const int c0 = count[0], c1 = c0 + count[1], c2 = c1 + count[2];
+    return i < c0 ? begin[0] + i : i < c1 ? begin[1] + i - c0 : i < c2 ? begin[2] + i - c1 : begin[3] + i - c2;
+  }
+};
+__device__ __forceinline__ Tiles tiles_of(const KvDev& kv, const KvAttendDev& at, const Block& b, int tile_tokens) {
+  const int64_t held = (int64_t)kv.table_stride << kv.page_shift;
+  const int end = kv.pool_pages ? (int)min(held, (int64_t)b.p_hi + 1) : 0;
+  int near = at.window ? (int)max((int64_t)0, (int64_t)b.p_lo - at.window + 1) : 0, sink = at.window ? min(at.n_sink, end) : 0;
+  if (near <= sink) near = sink = 0;         // the window reaches the first tokens
+  const int cut[4][2] = {{0, min(sink, b.hole_b)}, {max(0, b.hole_e), sink}, {near, min(end, b.hole_b)}, {max(near, b.hole_e), end}};
+  const bool hole = b.hole_e > b.hole_b;
+  Tiles t;
+  int last = 0;
+  t.total = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    int lo = cut[k][0], hi = cut[k][1];
+    if (!hole) {
+      if (k & 1) hi = lo;                    // one piece each
+      else hi = k == 0 ? sink : end;
+    }
+    t.begin[k] = max(last, max(lo, 0) / tile_tokens);
+    const int stop = hi > lo ? (hi - 1) / tile_tokens + 1 : 0;
+    t.count[k] = max(0, stop - t.begin[k]);
+    if (t.count[k] > 0) last = t.begin[k] + t.count[k];
+    t.total += t.count[k];
+  }
+  return t;
+}
+
+__device__ __forceinline__ bool sees(const KvAttendDev& at, const Block& b, int p, int j) {
+  return j <= p && (at.window == 0 || p - j < at.window || j < at.n_sink) && !(j >= b.hole_b && j < b.hole_e);
+}
+// does some row / does every row of the block see all tokens j0 .. j1?
+__device__ __forceinline__ bool all_see(const KvAttendDev& at, const Block& b, int j0, int j1) {
+  return j1 <= b.p_lo && (at.window == 0 || b.p_hi - j0 < at.window || j1 < at.n_sink) && (j1 < b.hole_b || j0 >= b.hole_e);
+}
+__device__ __forceinline__ bool one_sees(const KvAttendDev& at, const Block& b, int j) {
+  return j <= b.p_hi && (at.window == 0 || b.p_lo - j < at.window || j < at.n_sink) && !(j >= b.hole_b && j < b.hole_e);
+}
+
+// Base 2 logarithm of a sum's scale joined with the sum: what the caller gets is the natural one.
+__device__ __forceinline__ float row_lse(float m2, float l) {
+  return l > 0.f ? 0.69314718055994531f * m2 + __logf(l) : l != l ? l : -INFINITY;
+}
+// The maximum that goes with a partial sum.  A NaN score leaves a row's reference point at -infinity, and joining takes that for an
+// empty part: such a part says +infinity instead, and the row becomes NaN.
+__device__ __forceinline__ float part_max(float m, float l) { return m == -INFINITY && l != l ? INFINITY : m; }
+
+// Eight elements of a finished row (un-normalised sums o, maximum m2, sum l): joined with the caller's partial result and written.
+__device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int hq, int piece, const float (&o)[8], float m2, float l) {
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = o[i] * inv;
+  float lse = row_lse(m2, l);
+  const int64_t idx = tok * at.n_q_heads + hq;
+  if (at.other_out) {
+    const float pl = at.other_lse[idx];
+    if (pl != -INFINITY) {
+      const float top = fmaxf(lse, pl);
+      const float w = __expf(lse - top), pw = __expf(pl - top), both = w + pw;
+      const float* po = at.other_out + idx * kHeadDim + 8 * piece;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = (w * r[i] + pw * po[i]) / both;
+      lse = top + __logf(both);
+    }
+  }
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack2(r[2 * i], r[2 * i + 1]);
+  *reinterpret_cast<u32x4*>(at.out + tok * at.out_stride + hq * kRow + 16 * piece) = v;
+  if (at.lse && piece == 0) at.lse[idx] = lse;
+}
+
+// A tile's K and V as they lie in memory.  K: lane (n, g) = (lane % 16, lane / 16) holds token 16 tt + n; bf16: elements 32 kk + 8 g .. + 7 as
+// k[2 kk + tt]; 4 bits: elements 32 g .. + 31 (one block) as k[tt].  V: bf16: lane holds 16 bytes (lane % 16) of token 4 i + lane / 16;
+// 4 bits: block lane % 4 of token 16 i + lane / 4.
+template <bool FOUR>
+struct Raw {
+  u32x4 k[FOUR ? 2 : 8], v[FOUR ? 2 : 8];
+  uint32_t ke[2], ve[2];
+  int ok;                                    // bit tt: the page of tokens 16 tt .. is there
+};
+
+template <bool FOUR>
+__device__ __forceinline__ void load_tile(const KvDev& kv, const Block& b, int h, int tile, int lane, Raw<FOUR>& r) {
+  const int n = lane & 15, g = lane >> 4, T = 1 << kv.page_shift;
+  const int64_t j0 = (int64_t)tile * kTile;
+  int page[2];
+  page[0] = page_of(kv, b.s, j0 >> kv.page_shift);
+  page[1] = T == 32 ? page[0] : page_of(kv, b.s, (j0 >> kv.page_shift) + 1);
+  r.ok = (page[0] >= 0 ? 1 : 0) | (page[1] >= 0 ? 2 : 0);
+  const int second = T == 32 ? 16 : 0;       // first row of the tile's second half in its page
+  // (a page that is not there: page 0 is read in its place and what it holds is not seen)
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int64_t pg = max(page[tt], 0);
+    const int row0 = tt ? second : 0;
+    if constexpr (FOUR) {
+      const int64_t base = (pg * kv.heads + h) * (T * 68);
+      const char* k = kv.k + base;
+      const char* v = kv.v + base;
+      r.k[tt] = *reinterpret_cast<const u32x4*>(k + (row0 + n) * kRow4 + 16 * g);
+      r.ke[tt] = *reinterpret_cast<const uint8_t*>(k + T * kRow4 + (row0 + n) * 4 + g);
+      r.v[tt] = *reinterpret_cast<const u32x4*>(v + row0 * kRow4 + 16 * lane);
+      r.ve[tt] = *reinterpret_cast<const uint8_t*>(v + T * kRow4 + row0 * 4 + lane);
+    } else {
+      const int64_t base = (((pg << kv.page_shift) + row0) * kv.heads + h) * kRow;
+      const char* k = kv.k + base + n * kv.heads * kRow + 16 * g;
+      const char* v = kv.v + base + g * kv.heads * kRow + 16 * n;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) r.k[2 * kk + tt] = *reinterpret_cast<const u32x4*>(k + 64 * kk);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.v[4 * tt + i] = *reinterpret_cast<const u32x4*>(v + 4 * i * kv.heads * kRow);
+    }
+  }
+}
+
+__device__ __forceinline__ bool odd16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// V into LDS (row-major), tokens that no row of the block sees as zeros.  True: some row sees a token that another does not, and
+// V holds infinities or NaN, which a weight of zero would not silence.
+template <bool FOUR>
+__device__ __forceinline__ bool stage_v(const KvAttendDev& at, const Block& b, int tile, bool masked, int lane, Raw<FOUR>& r, uint16_t* Vs) {
+  bool odd = false;
+  if constexpr (FOUR) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = 16 * i + (lane >> 2);
+      if (masked && !((r.ok >> i & 1) && one_sees(at, b, tile * kTile + t))) {
+        r.v[i] = u32x4{0, 0, 0, 0};
+        r.ve[i] = 0;
+      }
+      odd |= r.ve[i] == 255;
+      u32x4* dst = reinterpret_cast<u32x4*>(Vs + t * kVsStride + 32 * (lane & 3));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dst[e] = from4(r.v[i][e], r.ve[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 4 * i + (lane >> 4);
+      if (masked) {
+        if (!((r.ok >> (i >> 2) & 1) && one_sees(at, b, tile * kTile + t))) r.v[i] = u32x4{0, 0, 0, 0};
+        odd |= odd16(r.v[i][0]) || odd16(r.v[i][1]) || odd16(r.v[i][2]) || odd16(r.v[i][3]);
+      }
+      *reinterpret_cast<u32x4*>(Vs + t * kVsStride + 8 * (lane & 15)) = r.v[i];
+    }
+  }
+  return masked && b.p_lo != b.p_hi && __any(odd);
+}
+
+// Running softmax of 16 query rows: lane (n, g) holds row n; its sum over the lane's own tokens, and elements 16 b + 4 g + i of the
+// un-normalised output.
+struct Rows16 {
+  float m, l;
+  f32x4 o[8];
+};
+
+// The part of V that is not finite, for the rows that see its token: weight times value, element by element.  p: the lane's weights
+// (tokens 16 tt + 4 g + i as p[4 tt + i]), -1 where the row does not see the token.  Rare, so small rather than fast.
+__device__ __forceinline__ void add_odd(const uint16_t* Vs, const float (&p)[8], int n, int g, Rows16& st) {
+  for (int gg = 0; gg < 4; ++gg)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = __shfl(p[k], n + 16 * gg);
+      const uint16_t* v = Vs + (16 * (k >> 2) + 4 * gg + (k & 3)) * kVsStride;
+      if (w < 0.f) continue;
+#pragma unroll
+      for (int b = 0; b < 8; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = lo16(v[16 * b + 4 * g + i]);
+          if (!(fabsf(x) < INFINITY)) st.o[b][i] += w * x;
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t finite16(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+
+// Few query rows (decoding, drafted tokens): a wavefront holds NR tiles of 16 rows and takes every fourth 32-token tile of the workgroup's
+// part; the four join at the end.  K goes from memory into the operands of the products as it lies there (S^T = K Q^T: lane (n, g) then
+// holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.
+template <bool FOUR, int NR>
+__global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
+  constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
+  __shared__ __align__(16) char lds[4 * kTile * kVsStride * 2];
+  __shared__ float ml[4][16][2];
+  static_assert(4 * 16 * kJoin * 4 <= 4 * kTile * kVsStride * 2, "the joining area lies over the V tiles");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % kv.heads;
+  const int rest = blockIdx.x / kv.heads, chunk = rest % at.n_chunks, id = rest / at.n_chunks;
+  Block b;
+  if (!find_block(kv, at, id, 16 * NR, lane, b)) return;
+  const Tiles tiles = tiles_of(kv, at, b, kTile);
+  const int t_begin = (int)((int64_t)tiles.total * chunk / at.n_chunks), t_end = (int)((int64_t)tiles.total * (chunk + 1) / at.n_chunks);
+
+  bf16x8 qf[NR][4];
+  int pos[NR];
+#pragma unroll
+  for (int rt = 0; rt < NR; ++rt) {
+    const int r = b.r0 + 16 * rt + n;
+    const bool on = r < b.n_rows;
+    const int t = (on ? r : b.r0) / at.group, hq = h * at.group + (on ? r : b.r0) % at.group;
+    pos[rt] = on ? b.pos0 + t : -1;
+    const char* q = at.q + (int64_t)(b.q0 + t) * at.q_stride + hq * kRow;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(q + (FOUR ? 64 * g + 16 * kk : 64 * kk + 16 * g));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = on ? (at.q_flip ? w[e] ^ 0x80008000u : w[e]) : 0u;
+      qf[rt][kk] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+  Rows16 st[NR];
+#pragma unroll
+  for (int rt = 0; rt < NR; ++rt) {
+    st[rt].m = -INFINITY;
+    st[rt].l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) st[rt].o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kVsStride;
+  Raw<FOUR> next;
+  if (t_begin + wave < t_end) load_tile<FOUR>(kv, b, h, tiles.tile(t_begin + wave), lane, next);
+  for (int i = t_begin + wave; i < t_end; i += 4) {
+    Raw<FOUR> cur = next;
+    const int tile = tiles.tile(i), j0 = tile * kTile;
+    if (i + 4 < t_end) load_tile<FOUR>(kv, b, h, tiles.tile(i + 4), lane, next);
+    const bool masked = cur.ok != 3 || !all_see(at, b, j0, j0 + kTile - 1);
+    wave_sync();
+    const bool odd = stage_v<FOUR>(at, b, tile, masked, lane, cur, Vs);
+    wave_sync();
+    f32x4 s[NR][2];
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        u32x4 kf;
+        if constexpr (FOUR) kf = from4(cur.k[tt][kk], cur.ke[tt]);
+        else kf = cur.k[2 * kk + tt];
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+          s[rt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[rt][kk], s[rt][tt], 0, 0, 0);
+      }
+    bf16x8 pb[NR];
+    float p[NR][8];
+#pragma unroll
+    for (int rt = 0; rt < NR; ++rt) {
+      uint32_t live = 255;
+      if (masked) {
+        live = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if ((cur.ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live |= 1u << k;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        p[rt][k] = (live >> k & 1) ? s[rt][k >> 2][k & 3] * at.scale2 : -INFINITY;
+        mx = fmaxf(mx, p[rt][k]);
+      }
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      // the reference point moves only where a score passes it by 2^8: until then the weights are at most that, in fp32 and bf16 alike
+      const float m_new = mx > st[rt].m + 8.f || st[rt].m == -INFINITY ? fmaxf(st[rt].m, mx) : st[rt].m;
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        p[rt][k] = __builtin_amdgcn_exp2f(p[rt][k] - ref);
+        sum += p[rt][k];
+      }
+      if (__any(m_new != st[rt].m)) {
+        const float alpha = __builtin_amdgcn_exp2f(st[rt].m - ref);
+        st[rt].l *= alpha;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) st[rt].o[e] *= alpha;
+      }
+      st[rt].l += sum;
+      st[rt].m = m_new;
+      u32x4 pw;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pw[e] = pack2(p[rt][2 * e], p[rt][2 * e + 1]);
+      pb[rt] = __builtin_bit_cast(bf16x8, pw);
+      if (odd)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) p[rt][k] = (live >> k & 1) ? p[rt][k] : -1.f;
+    }
+    const uint16_t* base = Vs + (4 * g + (n >> 2)) * kVsStride + 4 * (n & 3);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * e));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * kVsStride + 16 * e));
+      const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+      u32x4 a = {l2.x, l2.y, h2.x, h2.y};
+      if (odd)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = finite16(a[k]);
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt)
+        st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
+    }
+    if (odd)
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt) add_odd(Vs, p[rt], n, g, st[rt]);
+  }
+
+  // the four wavefronts' rows joined: 16 lanes per row, eight elements each
+  float (*join)[16][kJoin] = reinterpret_cast<float (*)[16][kJoin]>(lds);
+  const int row = threadIdx.x >> 4, piece = threadIdx.x & 15;
+#pragma unroll
+  for (int rt = 0; rt < NR; ++rt) {
+    __syncthreads();
+    float l = st[rt].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      ml[wave][n][0] = part_max(st[rt].m, l);
+      ml[wave][n][1] = l;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) *reinterpret_cast<f32x4*>(&join[wave][n][16 * e + 4 * g]) = st[rt].o[e];
+    __syncthreads();
+    const int r = b.r0 + 16 * rt + row;
+    if (r >= b.n_rows) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][row][0]);
+    float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float m = ml[w][row][0];
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      sum += f * ml[w][row][1];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] += f * join[w][row][8 * piece + k];
+    }
+    const int64_t tok = b.q0 + r / at.group;
+    const int hq = h * at.group + r % at.group;
+    if (at.n_chunks == 1) {
+      finish(at, tok, hq, piece, o, top, sum);
+    } else {
+      const int64_t part = (tok * at.n_q_heads + hq) * at.n_chunks + chunk;
+      *reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece) = f32x4{o[0], o[1], o[2], o[3]};
+      *reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece + 4) = f32x4{o[4], o[5], o[6], o[7]};
+      if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{top, sum};
+    }
+  }
+}
+
+// The chunks' results of a row joined: 16 lanes per row.
+__global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) {
+  const int64_t idx = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int piece = threadIdx.x & 15;
+  if (idx >= rows) return;
+  const int64_t tok = idx / at.n_q_heads;
+  if (tok < start_of(kv, 0) || tok >= start_of(kv, kv.n_seqs)) return;
+  const float* ml = at.part_ml + 2 * idx * at.n_chunks;
+  float top = -INFINITY;
+  for (int c = 0; c < at.n_chunks; ++c) top = fmaxf(top, part_max(ml[2 * c], ml[2 * c + 1]));
+  float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < at.n_chunks; ++c) {
+    const float m = part_max(ml[2 * c], ml[2 * c + 1]);
+    if (m == -INFINITY) continue;            // an empty part
+    const float f = __builtin_amdgcn_exp2f(m - top);
+    sum += f * ml[2 * c + 1];
+    const float* po = at.part_o + (idx * at.n_chunks + c) * kHeadDim + 8 * piece;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] += f * po[k];
+  }
+  finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
+}
+
+template <class... A>
+hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t st, A... args) {
+  void* p[] = {(void*)&args...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)blocks), dim3((unsigned)threads), p, 0, st);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
+  return launch(four ? tdk_kv_append_kernel<true> : tdk_kv_append_kernel<false>, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
+}
+
+hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
+  return launch(four ? tdk_kv_read_kernel<true> : tdk_kv_read_kernel<false>, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
+}
+
+hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st) {
+  const int64_t blocks = p.ids * kv.heads * p.n_chunks;
+  auto kernel = p.block_rows == 16 ? (four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>)
+                                   : (four ? tdk_kv_attend_rows_kernel<true, 2> : tdk_kv_attend_rows_kernel<false, 2>);
+  hipError_t e = launch(kernel, blocks, 256, st, kv, at);
+  if (e == hipSuccess && p.n_chunks > 1) e = launch(tdk_kv_attend_join_kernel, (p.rows + 15) / 16, 256, st, kv, at, p.rows);
+  return e;
+}
+
+}  // namespace tdk

@@ -19,6 +19,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_HIP, ERR_NOMEM = range(6
 BF16 = 0
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 PLANE_K, PLANE_V = 1, 2
+KV_BF16, KV_MXFP4 = 0, 1
 (KERNEL_REROTATE, KERNEL_FLAG, KERNEL_COMPACT, KERNEL_GATHER, KERNEL_DECODE, KERNEL_SCATTER,
  KERNEL_KEYDIFF, KERNEL_SELECT, KERNEL_MASTER, KERNEL_ATTEND_QROT, KERNEL_ATTEND_MASTER, KERNEL_ATTEND_DIFF,
  KERNEL_ATTEND_MERGE) = range(13)
@@ -36,6 +37,8 @@ EXPORTS = (
     "tdk_diff_encode_plane", "tdk_diff_decode_plane", "tdk_attend_workspace_bytes", "tdk_attend_shared",
     "tdk_prompt_plan_create", "tdk_prompt_plan_destroy", "tdk_prompt_plan_n_sessions", "tdk_prompt_plan_span",
     "tdk_prompt_plan_session_of", "tdk_prompt_plan_segments",
+    "tdk_kv_create", "tdk_kv_destroy", "tdk_kv_page_bytes", "tdk_kv_append", "tdk_kv_read",
+    "tdk_kv_attend_workspace_bytes", "tdk_kv_attend",
     "tdk_timing_enable", "tdk_timing_read", "tdk_timing_reset",
     "tdk_dense_bytes", "tdk_diff_bytes", "tdk_family_cost",
     "tdk_util_copy", "tdk_util_fill", "tdk_util_page_fill", "tdk_util_page_read",
@@ -91,6 +94,27 @@ class PingPong(C.Structure):
     _fields_ = [("stage_k", C.c_void_p * 2), ("stage_v", C.c_void_p * 2), ("stage_bytes", C.c_size_t)]
 
 
+class KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pool_pages", C.c_int64)]
+
+
+class KvBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_len", C.c_int32), ("q_start", C.c_void_p),
+                ("seq_len", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int32)]
+
+
+class KvRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q", C.c_void_p),
+                ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("q_out", C.c_void_p), ("q_out_stride", C.c_int64)]
+
+
+class KvAttendIO(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("scale", C.c_float), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("window", C.c_int32), ("n_sink", C.c_int32), ("hole", C.c_void_p), ("part_out", C.c_void_p),
+                ("part_lse", C.c_void_p)]
+
+
 class TdkError(RuntimeError):
     def __init__(self, status: int, what: str, detail: str):
         super().__init__(f"{what}: status {status} ({detail})")
@@ -144,6 +168,16 @@ def load() -> C.CDLL:
     L.tdk_prompt_plan_segments.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.POINTER(Segment))]
     L.tdk_restore_layers.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                      C.POINTER(LayerIO), C.POINTER(Diff), C.POINTER(PingPong), C.c_void_p, C.c_void_p]
+    L.tdk_kv_create.argtypes = [C.POINTER(Model), C.c_int32, C.POINTER(C.c_void_p)]
+    L.tdk_kv_destroy.argtypes = [C.c_void_p]
+    L.tdk_kv_destroy.restype = None
+    L.tdk_kv_page_bytes.argtypes = [C.c_void_p]
+    L.tdk_kv_page_bytes.restype = C.c_size_t
+    L.tdk_kv_append.argtypes = [C.c_void_p, C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(KvRows), C.c_void_p]
+    L.tdk_kv_read.argtypes = L.tdk_kv_append.argtypes
+    L.tdk_kv_attend_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(KvBatch), C.c_int32]
+    L.tdk_kv_attend_workspace_bytes.restype = C.c_size_t
+    L.tdk_kv_attend.argtypes = [C.c_void_p, C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(KvAttendIO), C.c_void_p]
     L.tdk_timing_enable.argtypes = [C.c_void_p, C.c_int32]
     L.tdk_timing_read.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     L.tdk_timing_reset.argtypes = [C.c_void_p]
@@ -380,6 +414,74 @@ def tdk_diff_encode_plane(r: Round, layer: int, io: LayerIO, eps: float, plane: 
 def tdk_diff_decode_plane(r: Round, layer: int, io: LayerIO, plane: int, d: Diff, stream: int = 0) -> None:
     _check(load().tdk_diff_decode_plane(r.handle, layer, C.byref(io), plane, C.byref(d), C.c_void_p(stream)),
            "tdk_diff_decode_plane")
+
+
+class Kv:
+    """Owns a tdk_kv handle."""
+
+    def __init__(self, handle: int):
+        self.handle = C.c_void_p(handle)
+
+    def destroy(self) -> None:
+        if self.handle:
+            load().tdk_kv_destroy(self.handle)
+            self.handle = C.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def tdk_kv_create(mdl: Model, fmt: int = KV_BF16) -> Kv:
+    out = C.c_void_p()
+    _check(load().tdk_kv_create(C.byref(mdl), int(fmt), C.byref(out)), "tdk_kv_create")
+    return Kv(out.value)
+
+
+def tdk_kv_destroy(kv: Kv) -> None:
+    kv.destroy()
+
+
+def tdk_kv_page_bytes(kv: Kv) -> int:
+    return int(load().tdk_kv_page_bytes(kv.handle))
+
+
+def kv_cache(k, v, pool_pages: int) -> KvCache:
+    return KvCache(_ptr(k), _ptr(v), int(pool_pages))
+
+
+def kv_batch(n_seqs: int, n_tokens: int, max_len: int, q_start, seq_len, block_table, table_stride: int) -> KvBatch:
+    return KvBatch(int(n_seqs), int(n_tokens), int(max_len), _ptr(q_start), _ptr(seq_len), _ptr(block_table), int(table_stride))
+
+
+def kv_rows(k, v, k_stride: int, v_stride: int, q=None, q_stride: int = 0, n_q_heads: int = 0, q_out=None,
+            q_out_stride: int = 0) -> KvRows:
+    return KvRows(_ptr(k), _ptr(v), int(k_stride), int(v_stride), _ptr(q), int(q_stride), int(n_q_heads), _ptr(q_out),
+                  int(q_out_stride))
+
+
+def tdk_kv_append(kv: Kv, cache: KvCache, batch: KvBatch, rows: KvRows, stream: int = 0) -> None:
+    _check(load().tdk_kv_append(kv.handle, C.byref(cache), C.byref(batch), C.byref(rows), C.c_void_p(stream)), "tdk_kv_append")
+
+
+def tdk_kv_read(kv: Kv, cache: KvCache, batch: KvBatch, rows: KvRows, stream: int = 0) -> None:
+    _check(load().tdk_kv_read(kv.handle, C.byref(cache), C.byref(batch), C.byref(rows), C.c_void_p(stream)), "tdk_kv_read")
+
+
+def kv_attend_io(q, q_stride: int, n_q_heads: int, scale: float, out, out_stride: int, lse, workspace, workspace_bytes: int,
+                 window: int = 0, n_sink: int = 0, hole=None, part_out=None, part_lse=None) -> KvAttendIO:
+    return KvAttendIO(_ptr(q), int(q_stride), int(n_q_heads), float(scale), _ptr(out), int(out_stride), _ptr(lse), _ptr(workspace),
+                      int(workspace_bytes), int(window), int(n_sink), _ptr(hole), _ptr(part_out), _ptr(part_lse))
+
+
+def tdk_kv_attend_workspace_bytes(kv: Kv, batch: KvBatch, n_q_heads: int) -> int:
+    return int(load().tdk_kv_attend_workspace_bytes(kv.handle, C.byref(batch), int(n_q_heads)))
+
+
+def tdk_kv_attend(kv: Kv, cache: KvCache, batch: KvBatch, a: KvAttendIO, stream: int = 0) -> None:
+    _check(load().tdk_kv_attend(kv.handle, C.byref(cache), C.byref(batch), C.byref(a), C.c_void_p(stream)), "tdk_kv_attend")
 
 
 def tdk_timing_enable(r: Round, on: bool) -> None:
