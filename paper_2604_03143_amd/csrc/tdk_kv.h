@@ -14,7 +14,7 @@ namespace tdk {
 struct KvDev {
   char*          k;
   char*          v;
-  int64_t        pool_pages;
+  int32_t        pool_pages;
   const int32_t* q_start;
   const int32_t* seq_len;
   const int32_t* table;

@@ -1,16 +1,17 @@
 // Caches that programs append to: new tokens into the pages (rotated on the way, in bf16 or in 4 bits), attention of their
 // queries to the pages, and rows back out of them.
 #include "tdk_kv.h"
+#include "tdk_internal.h"
 
-#include <algorithm>
+#include <type_traits>
 
 namespace tdk {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -267,18 +268,18 @@ __device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& a
   const auto first = [&](int i) { return (int64_t)start_of(kv, i) * at.group / block_rows + i; };
   b.s = count_up_to(first, kv.n_seqs, id, lane) - 1;
   if (b.s < 0) return false;
-  b.q0 = start_of(kv, b.s);
-  const int n = start_of(kv, b.s + 1) - b.q0;
+  b.q0 = min(max(scalar_read(kv.q_start + b.s), 0), kv.n_tokens);
+  const int n = min(max(scalar_read(kv.q_start + b.s + 1), 0), kv.n_tokens) - b.q0;
   if (n <= 0) return false;
   b.n_rows = n * at.group;                   // (at most n_tokens * n_q_heads, which the host has checked)
   const int64_t r0 = (id - first(b.s)) * block_rows;
   if (r0 >= b.n_rows) return false;
   b.r0 = (int)r0;
-  b.pos0 = max(kv.seq_len[b.s], 0) - n;      // (tokens of a call and of a table are at most 2^30: differences of positions fit)
+  b.pos0 = max(scalar_read(kv.seq_len + b.s), 0) - n;      // (tokens of a call and of a table are at most 2^30: differences of positions fit)
   b.p_lo = b.pos0 + b.r0 / at.group;
   b.p_hi = b.pos0 + (min(b.r0 + block_rows, b.n_rows) - 1) / at.group;
-  b.hole_b = at.hole ? at.hole[2 * b.s] : 0;
-  b.hole_e = at.hole ? max(at.hole[2 * b.s + 1], b.hole_b) : 0;
+  b.hole_b = at.hole ? scalar_read(at.hole + 2 * b.s) : 0;
+  b.hole_e = at.hole ? max(scalar_read(at.hole + 2 * b.s + 1), b.hole_b) : 0;
   return true;
 }
 
@@ -362,6 +363,42 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
   if (at.lse && piece == 0) at.lse[idx] = lse;
 }
 
+// The same for a workgroup's part: finished if it is the only one, else kept for the join.
+__device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m2, float l) {
+  if (at.n_chunks == 1) {
+    finish(at, tok, hq, piece, o, m2, l);
+    return;
+  }
+  const int64_t part = (tok * at.n_q_heads + hq) * at.n_chunks + chunk;
+  f32x4* dst = reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece);
+  dst[0] = f32x4{o[0], o[1], o[2], o[3]};
+  dst[1] = f32x4{o[4], o[5], o[6], o[7]};
+  if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{m2, l};
+}
+
+// Physical pages of the 16-token groups of a tile, -1 where there is none.  What follows is the same for the whole wavefront: scalar reads.
+template <int N>
+struct Pages { int p[N]; };
+template <int N>
+__device__ __forceinline__ Pages<N> pages_of(const KvDev& kv, int s, int tile) {
+  Pages<N> o;
+  const int32_t* row = kv.table + (int64_t)s * kv.table_stride;
+#pragma unroll
+  for (int it = 0; it < N; ++it) {
+    const int lp = (16 * N * tile + 16 * it) >> kv.page_shift;
+    const int v = scalar_read(row + min(lp, kv.table_stride - 1));
+    o.p[it] = lp < kv.table_stride && v < kv.pool_pages ? max(v, -1) : -1;
+  }
+  return o;
+}
+template <int N>
+__device__ __forceinline__ int there(const Pages<N>& pg) {      // bit it: the page of tokens 16 it .. is there
+  int ok = 0;
+#pragma unroll
+  for (int it = 0; it < N; ++it) ok |= (pg.p[it] >= 0 ? 1 : 0) << it;
+  return ok;
+}
+
 // A tile's K and V as they lie in memory.  K: lane (n, g) = (lane % 16, lane / 16) holds token 16 tt + n; bf16: elements 32 kk + 8 g .. + 7 as
 // k[2 kk + tt]; 4 bits: elements 32 g .. + 31 (one block) as k[tt].  V: bf16: lane holds 16 bytes (lane % 16) of token 4 i + lane / 16;
 // 4 bits: block lane % 4 of token 16 i + lane / 4.
@@ -373,31 +410,26 @@ struct Raw {
 };
 
 template <bool FOUR>
-__device__ __forceinline__ void load_tile(const KvDev& kv, const Block& b, int h, int tile, int lane, Raw<FOUR>& r) {
+__device__ __forceinline__ void load_tile(const KvDev& kv, const Pages<2>& pg, int h, int lane, Raw<FOUR>& r) {
   const int n = lane & 15, g = lane >> 4, T = 1 << kv.page_shift;
-  const int64_t j0 = (int64_t)tile * kTile;
-  int page[2];
-  page[0] = page_of(kv, b.s, j0 >> kv.page_shift);
-  page[1] = T == 32 ? page[0] : page_of(kv, b.s, (j0 >> kv.page_shift) + 1);
-  r.ok = (page[0] >= 0 ? 1 : 0) | (page[1] >= 0 ? 2 : 0);
-  const int second = T == 32 ? 16 : 0;       // first row of the tile's second half in its page
+  r.ok = there(pg);
   // (a page that is not there: page 0 is read in its place and what it holds is not seen)
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
-    const int64_t pg = max(page[tt], 0);
-    const int row0 = tt ? second : 0;
+    const int64_t page = max(pg.p[tt], 0);
+    const int row0 = 16 * tt & (T - 1);
     if constexpr (FOUR) {
-      const int64_t base = (pg * kv.heads + h) * (T * 68);
+      const int64_t base = (page * kv.heads + h) * (T * 68);
       const char* k = kv.k + base;
       const char* v = kv.v + base;
-      r.k[tt] = *reinterpret_cast<const u32x4*>(k + (row0 + n) * kRow4 + 16 * g);
-      r.ke[tt] = *reinterpret_cast<const uint8_t*>(k + T * kRow4 + (row0 + n) * 4 + g);
+      r.k[tt] = *reinterpret_cast<const u32x4*>(k + row0 * kRow4 + (n * kRow4 + 16 * g));
+      r.ke[tt] = *reinterpret_cast<const uint8_t*>(k + (T * kRow4 + row0 * 4) + (n * 4 + g));
       r.v[tt] = *reinterpret_cast<const u32x4*>(v + row0 * kRow4 + 16 * lane);
-      r.ve[tt] = *reinterpret_cast<const uint8_t*>(v + T * kRow4 + row0 * 4 + lane);
+      r.ve[tt] = *reinterpret_cast<const uint8_t*>(v + (T * kRow4 + row0 * 4) + lane);
     } else {
-      const int64_t base = (((pg << kv.page_shift) + row0) * kv.heads + h) * kRow;
-      const char* k = kv.k + base + n * kv.heads * kRow + 16 * g;
-      const char* v = kv.v + base + g * kv.heads * kRow + 16 * n;
+      const int64_t base = (((page << kv.page_shift) + row0) * kv.heads + h) * kRow;
+      const char* k = kv.k + base + (n * kv.heads * kRow + 16 * g);
+      const char* v = kv.v + base + (g * kv.heads * kRow + 16 * n);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) r.k[2 * kk + tt] = *reinterpret_cast<const u32x4*>(k + 64 * kk);
 #pragma unroll
@@ -447,34 +479,30 @@ struct Rows16 {
   f32x4 o[8];
 };
 
-// The part of V that is not finite, for the rows that see its token: weight times value, element by element.  p: the lane's weights
-// (tokens 16 tt + 4 g + i as p[4 tt + i]), -1 where the row does not see the token.  Rare, so small rather than fast.
-__device__ __forceinline__ void add_odd(const uint16_t* Vs, const float (&p)[8], int n, int g, Rows16& st) {
-  for (int gg = 0; gg < 4; ++gg)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float w = __shfl(p[k], n + 16 * gg);
-      const uint16_t* v = Vs + (16 * (k >> 2) + 4 * gg + (k & 3)) * kVsStride;
-      if (w < 0.f) continue;
-#pragma unroll
-      for (int b = 0; b < 8; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = lo16(v[16 * b + 4 * g + i]);
-          if (!(fabsf(x) < INFINITY)) st.o[b][i] += w * x;
-        }
-    }
+// V with what is not finite as zeros, and where it is +infinity, -infinity and NaN (ones).  Rows of the block differ in what they see, and a weight
+// of zero does not silence infinity or NaN: such a tile's products take the finite part of V, and what the rest does to the rows that
+// see it follows from products with these masks.  Rare, so small rather than fast.
+constexpr uint32_t kOne = 0x3f80u;         // bf16
+__device__ __forceinline__ uint32_t kind16(uint32_t v, int kind) {      // 0: finite part; 1, 2, 3: masks
+  const bool odd = (v & 0x7f80u) == 0x7f80u, inf = odd && (v & 0x7fu) == 0;
+  if (kind == 0) return odd ? 0u : v;
+  if (kind == 3) return odd && !inf ? kOne : 0u;
+  return inf && ((v >> 15) == 1u) == (kind == 2) ? kOne : 0u;
 }
-
-__device__ __forceinline__ uint32_t finite16(uint32_t w) {
-  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+__device__ __forceinline__ u32x4 kind_of(u32x4 v, int kind) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = kind16(v[k] & 0xffffu, kind) | kind16(v[k] >> 16, kind) << 16;
+  return v;
 }
+__device__ __forceinline__ float value_of(int kind) { return kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __uint_as_float(0x7fc00000u); }
+// ones for the tokens 2 e, 2 e + 1 of a lane that its row sees
+__device__ __forceinline__ uint32_t ones(uint32_t live, int e) { return (live >> (2 * e) & 1u ? kOne : 0u) | (live >> (2 * e + 1) & 1u ? kOne << 16 : 0u); }
 
 // Few query rows (decoding, drafted tokens): a wavefront holds NR tiles of 16 rows and takes every fourth 32-token tile of the workgroup's
 // part; the four join at the end.  K goes from memory into the operands of the products as it lies there (S^T = K Q^T: lane (n, g) then
 // holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.
 template <bool FOUR, int NR>
-__global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
   constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
   __shared__ __align__(16) char lds[4 * kTile * kVsStride * 2];
   __shared__ float ml[4][16][2];
@@ -515,11 +543,16 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv,
 
   uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kVsStride;
   Raw<FOUR> next;
-  if (t_begin + wave < t_end) load_tile<FOUR>(kv, b, h, tiles.tile(t_begin + wave), lane, next);
+  Pages<2> pages{};
+  if (t_begin + wave < t_end) {
+    load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(t_begin + wave)), h, lane, next);
+    if (t_begin + wave + 4 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(t_begin + wave + 4));
+  }
   for (int i = t_begin + wave; i < t_end; i += 4) {
     Raw<FOUR> cur = next;
     const int tile = tiles.tile(i), j0 = tile * kTile;
-    if (i + 4 < t_end) load_tile<FOUR>(kv, b, h, tiles.tile(i + 4), lane, next);
+    if (i + 4 < t_end) load_tile<FOUR>(kv, pages, h, lane, next);
+    if (i + 8 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(i + 8));
     const bool masked = cur.ok != 3 || !all_see(at, b, j0, j0 + kTile - 1);
     wave_sync();
     const bool odd = stage_v<FOUR>(at, b, tile, masked, lane, cur, Vs);
@@ -539,21 +572,21 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv,
           s[rt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[rt][kk], s[rt][tt], 0, 0, 0);
       }
     bf16x8 pb[NR];
-    float p[NR][8];
+    uint32_t live[NR];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
-      uint32_t live = 255;
+      live[rt] = 255;
       if (masked) {
-        live = 0;
+        live[rt] = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if ((cur.ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live |= 1u << k;
+          if ((cur.ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live[rt] |= 1u << k;
       }
-      float mx = -INFINITY;
+      float p[8], mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        p[rt][k] = (live >> k & 1) ? s[rt][k >> 2][k & 3] * at.scale2 : -INFINITY;
-        mx = fmaxf(mx, p[rt][k]);
+        p[k] = (live[rt] >> k & 1) ? s[rt][k >> 2][k & 3] * at.scale2 : -INFINITY;
+        mx = fmaxf(mx, p[k]);
       }
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -563,8 +596,8 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv,
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        p[rt][k] = __builtin_amdgcn_exp2f(p[rt][k] - ref);
-        sum += p[rt][k];
+        p[k] = __builtin_amdgcn_exp2f(p[k] - ref);
+        sum += p[k];
       }
       if (__any(m_new != st[rt].m)) {
         const float alpha = __builtin_amdgcn_exp2f(st[rt].m - ref);
@@ -576,29 +609,39 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv,
       st[rt].m = m_new;
       u32x4 pw;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pw[e] = pack2(p[rt][2 * e], p[rt][2 * e + 1]);
+      for (int e = 0; e < 4; ++e) pw[e] = pack2(p[2 * e], p[2 * e + 1]);
       pb[rt] = __builtin_bit_cast(bf16x8, pw);
-      if (odd)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) p[rt][k] = (live >> k & 1) ? p[rt][k] : -1.f;
     }
     const uint16_t* base = Vs + (4 * g + (n >> 2)) * kVsStride + 4 * (n & 3);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    const auto operand = [&](int e) {        // V^T: element 16 e + n of tokens 4 g .. + 3 and 16 + 4 g .. + 3
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * e));
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * kVsStride + 16 * e));
       const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-      u32x4 a = {l2.x, l2.y, h2.x, h2.y};
-      if (odd)
+      return u32x4{l2.x, l2.y, h2.x, h2.y};
+    };
+    if (!odd) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] = finite16(a[k]);
+      for (int e = 0; e < 8; ++e) {
+        const u32x4 a = operand(e);
 #pragma unroll
-      for (int rt = 0; rt < NR; ++rt)
-        st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
+        for (int rt = 0; rt < NR; ++rt)
+          st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
+      }
+      continue;
     }
-    if (odd)
 #pragma unroll
-      for (int rt = 0; rt < NR; ++rt) add_odd(Vs, p[rt], n, g, st[rt]);
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt) {
+        st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kind_of(operand(e), 0)), pb[rt], st[rt].o[e], 0, 0, 0);
+        const u32x4 see = {ones(live[rt], 0), ones(live[rt], 1), ones(live[rt], 2), ones(live[rt], 3)};
+        for (int kind = 1; kind <= 3; ++kind) {
+          const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kind_of(operand(e), kind)),
+                                                                     __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st[rt].o[e][i] += hit[i] > 0.f ? value_of(kind) : 0.f;
+        }
+      }
   }
 
   // the four wavefronts' rows joined: 16 lanes per row, eight elements each
@@ -631,16 +674,288 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_rows_kernel(const KvDev kv,
 #pragma unroll
       for (int k = 0; k < 8; ++k) o[k] += f * join[w][row][8 * piece + k];
     }
-    const int64_t tok = b.q0 + r / at.group;
-    const int hq = h * at.group + r % at.group;
-    if (at.n_chunks == 1) {
-      finish(at, tok, hq, piece, o, top, sum);
-    } else {
-      const int64_t part = (tok * at.n_q_heads + hq) * at.n_chunks + chunk;
-      *reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece) = f32x4{o[0], o[1], o[2], o[3]};
-      *reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece + 4) = f32x4{o[4], o[5], o[6], o[7]};
-      if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{top, sum};
+    put_row(at, b.q0 + r / at.group, h * at.group + r % at.group, chunk, piece, o, top, sum);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS, two stages of them: the next step's
+// pages are on their way into registers while this one's products run, and go into the other stage behind them.
+// ---------------------------------------------------------------------------------------------
+constexpr int kStep = 64;                  // tokens per step of a workgroup
+constexpr int kKsStride = kHeadDim + 8;    // bf16 elements per staged K row (+16 bytes: spreads LDS banks)
+constexpr int kStageK = kStep * kKsStride, kStage = kStageK + kStep * kVsStride;      // elements
+
+// A step's K and V on their way: bf16: 16 bytes (thread % 16) of tokens 16 it + thread / 16; 4 bits: block thread % 4 of token thread / 4.
+template <bool FOUR>
+struct RawStep {
+  u32x4 k[FOUR ? 1 : 4], v[FOUR ? 1 : 4];
+  uint32_t ke, ve;
+};
+
+template <bool FOUR>
+__device__ __forceinline__ void load_step(const KvDev& kv, const Pages<4>& pg, int h, int wave, RawStep<FOUR>& r) {
+  const int tid = threadIdx.x, lane = tid & 63, T = 1 << kv.page_shift;
+  if constexpr (FOUR) {
+    const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
+    const int row0 = 16 * wave & (T - 1);
+    const int64_t base = (page * kv.heads + h) * (T * 68);
+    r.k[0] = *reinterpret_cast<const u32x4*>(kv.k + base + row0 * kRow4 + 16 * lane);
+    r.ke = *reinterpret_cast<const uint8_t*>(kv.k + base + (T * kRow4 + row0 * 4) + lane);
+    r.v[0] = *reinterpret_cast<const u32x4*>(kv.v + base + row0 * kRow4 + 16 * lane);
+    r.ve = *reinterpret_cast<const uint8_t*>(kv.v + base + (T * kRow4 + row0 * 4) + lane);
+  } else {
+    const int lane_off = (tid >> 4) * kv.heads * kRow + 16 * (tid & 15);
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int64_t base = ((((int64_t)max(pg.p[it], 0) << kv.page_shift) + (16 * it & (T - 1))) * kv.heads + h) * kRow;
+      r.k[it] = *reinterpret_cast<const u32x4*>(kv.k + base + lane_off);
+      r.v[it] = *reinterpret_cast<const u32x4*>(kv.v + base + lane_off);
     }
+  }
+}
+
+// Into a stage.  masked: some row of the block does not see some token; then tokens that none sees become zeros in V, and the wavefront's entry
+// of `odd` says whether what is left holds infinities or NaN.
+template <bool FOUR>
+__device__ __forceinline__ void store_step(const KvAttendDev& at, const Block& b, int tile, int ok, bool masked, RawStep<FOUR>& r, uint16_t* stage, int* odd) {
+  const int tid = threadIdx.x;
+  bool strange = false;
+  if constexpr (FOUR) {
+    const int t = tid >> 2, c = 32 * (tid & 3);
+    if (masked) {
+      if (!((ok >> (t >> 4) & 1) && one_sees(at, b, tile * kStep + t))) { r.v[0] = u32x4{0, 0, 0, 0}; r.ve = 0; }
+      strange = r.ve == 255;
+    }
+    u32x4* dk = reinterpret_cast<u32x4*>(stage + t * kKsStride + c);
+    u32x4* dv = reinterpret_cast<u32x4*>(stage + kStageK + t * kVsStride + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      dk[e] = from4(r.k[0][e], r.ke);
+      dv[e] = from4(r.v[0][e], r.ve);
+    }
+  } else {
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int t = 16 * it + (tid >> 4), c = 8 * (tid & 15);
+      if (masked) {
+        if (!((ok >> it & 1) && one_sees(at, b, tile * kStep + t))) r.v[it] = u32x4{0, 0, 0, 0};
+        strange |= odd16(r.v[it][0]) || odd16(r.v[it][1]) || odd16(r.v[it][2]) || odd16(r.v[it][3]);
+      }
+      *reinterpret_cast<u32x4*>(stage + t * kKsStride + c) = r.k[it];
+      *reinterpret_cast<u32x4*>(stage + kStageK + t * kVsStride + c) = r.v[it];
+    }
+  }
+  if (masked) {
+    const int any = __any(strange);
+    if ((tid & 63) == 0) odd[tid >> 6] = any;
+  }
+}
+
+// Running softmax of 32 query rows: lane (n, hh) = (lane % 32, lane / 32) holds row n, elements 32 b + 8 (i / 4) + 4 hh + i % 4 of it.
+struct Rows32 {
+  float m, l;
+  f32x16 o[4];
+};
+
+// O^T += V^T P^T for a step.  p[i]: the weight of token 32 (i / 16) + 8 ((i % 16) / 4) + 4 hh + i % 4.  Within 16 lanes a transposing read takes
+// the lanes' 8-byte pieces as the rows of a 16 x 4 matrix and hands lane i its column: with lane i at (token i / 4, four elements i % 4) it
+// gets element i of the four tokens.
+__device__ __forceinline__ u32x4 operand_v(const uint16_t* Vs, int kk, int e, int lane) {
+  const int i16 = lane & 15, blk = lane >> 4;
+  const uint16_t* at = Vs + (4 * (blk >> 1) + (i16 >> 2)) * kVsStride + 16 * (blk & 1) + 4 * (i16 & 3) + 16 * kk * kVsStride + 32 * e;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * kVsStride));
+  const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+  return u32x4{l2.x, l2.y, h2.x, h2.y};
+}
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ void products_v(const uint16_t* Vs, const u32x4 (&pw)[4], int lane, Rows32& st) {
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) st.o[e] = mfma32(operand_v(Vs, kk, e, lane), pw[kk], st.o[e]);
+}
+// The same where V holds what only some of the rows may meet (kind_of); bit i of live: the row sees token i of the lane's 32.
+__device__ __forceinline__ void products_odd(const uint16_t* Vs, const u32x4 (&pw)[4], uint32_t live, int lane, Rows32& st) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) st.o[e] = mfma32(kind_of(operand_v(Vs, kk, e, lane), 0), pw[kk], st.o[e]);
+    for (int kind = 1; kind <= 3; ++kind) {
+      f32x16 hit;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+      for (int kk = 0; kk < 4; ++kk) {
+        const uint32_t l8 = live >> (8 * kk);
+        hit = mfma32(kind_of(operand_v(Vs, kk, e, lane), kind), u32x4{ones(l8, 0), ones(l8, 1), ones(l8, 2), ones(l8, 3)}, hit);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[e][i] += hit[i] > 0.f ? value_of(kind) : 0.f;
+    }
+  }
+}
+
+template <bool FOUR>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_tile_kernel(const KvDev kv, const KvAttendDev at,
+                                                                                                            const int last_id) {
+  constexpr int kJoin = kHeadDim + 4;        // floats per row of the area that turns the results
+  __shared__ __align__(16) uint16_t lds[2 * kStage];
+  __shared__ int odd_at[2][4];
+  static_assert(4 * 32 * kJoin * 4 <= 2 * kStage * 2, "the turning area lies over the stages");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hh = lane >> 5;
+  const int h = blockIdx.x % kv.heads;
+  const int rest = blockIdx.x / kv.heads, chunk = rest % at.n_chunks;
+  Block b;
+  // (a causal prompt's last rows see most: they start first)
+  if (!find_block(kv, at, last_id - rest / at.n_chunks, 128, lane, b)) return;
+  const Tiles tiles = tiles_of(kv, at, b, kStep);
+  const int t_begin = (int)((int64_t)tiles.total * chunk / at.n_chunks), t_end = (int)((int64_t)tiles.total * (chunk + 1) / at.n_chunks);
+  // the wavefront's own rows
+  Block w = b;
+  w.r0 = b.r0 + 32 * wave;
+  const bool any_row = w.r0 < b.n_rows;
+  w.p_lo = b.pos0 + w.r0 / at.group;
+  w.p_hi = b.pos0 + (min(w.r0 + 32, b.n_rows) - 1) / at.group;
+
+  bf16x8 qf[8];
+  const int r = w.r0 + n;
+  const bool on = r < b.n_rows;
+  const int pos = on ? b.pos0 + r / at.group : -1;
+  {
+    const int rr = on ? r : b.r0;
+    const char* q = at.q + (int64_t)(b.q0 + rr / at.group) * at.q_stride + (h * at.group + rr % at.group) * kRow;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      u32x4 x = *reinterpret_cast<const u32x4*>(q + 32 * kk + 16 * hh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = on ? (at.q_flip ? x[e] ^ 0x80008000u : x[e]) : 0u;
+      qf[kk] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  Rows32 st;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st.o[e][i] = 0.f;
+
+  RawStep<FOUR> raw;
+  Pages<4> pages{};
+  int ok = 0;
+  bool masked = false;
+  if (t_begin < t_end) {
+    const int tile = tiles.tile(t_begin);
+    pages = pages_of<4>(kv, b.s, tile);
+    ok = there(pages);
+    load_step<FOUR>(kv, pages, h, wave, raw);
+    if (t_begin + 1 < t_end) pages = pages_of<4>(kv, b.s, tiles.tile(t_begin + 1));
+    masked = ok != 15 || !all_see(at, b, tile * kStep, tile * kStep + kStep - 1);
+    store_step<FOUR>(at, b, tile, ok, masked, raw, lds, odd_at[0]);
+  }
+  __syncthreads();
+  for (int i = t_begin; i < t_end; ++i) {
+    const int cur = (i - t_begin) & 1;
+    const int tile = tiles.tile(i), j0 = tile * kStep;
+    const int next = i + 1 < t_end ? tiles.tile(i + 1) : 0;
+    const int ok_next = there(pages);
+    if (i + 1 < t_end) load_step<FOUR>(kv, pages, h, wave, raw);
+    if (i + 2 < t_end) pages = pages_of<4>(kv, b.s, tiles.tile(i + 2));
+    const uint16_t* Ks = lds + cur * kStage;
+    const uint16_t* Vs = Ks + kStageK;
+    // (does some row of the wavefront see some token of the step?)
+    const bool some = any_row && j0 <= w.p_hi && (at.window == 0 || w.p_lo - (j0 + kStep - 1) < at.window || j0 < at.n_sink);
+    if (some) {
+      f32x16 s[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(Ks + (32 * tt + n) * kKsStride + 16 * kk + 8 * hh);
+          s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qf[kk], s[tt], 0, 0, 0);
+        }
+      float p[32];
+#pragma unroll
+      for (int k = 0; k < 32; ++k) p[k] = s[k >> 4][k & 15];
+      const bool own_mask = masked && (ok != 15 || !all_see(at, w, j0, j0 + kStep - 1));
+      uint32_t live = ~0u;
+      if (own_mask) {
+        const int a = pos - j0 - 4 * hh, lo = at.window ? a - at.window : -1, sink = at.n_sink - j0 - 4 * hh;
+        const int hb = b.hole_b - j0 - 4 * hh, he = b.hole_e - j0 - 4 * hh;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const int t = 32 * (k >> 4) + 8 * ((k & 15) >> 2) + (k & 3);
+          const bool see = t <= a && (at.window == 0 || t > lo || t < sink) && !(t >= hb && t < he) && (ok >> (t >> 4) & 1);
+          p[k] = see ? p[k] : -INFINITY;
+          live = see ? live : live & ~(1u << k);
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(p[k], p[k + 1]));
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * at.scale2;
+      // the reference point moves only where a score passes it by 2^8: until then the weights are at most that, in fp32 and bf16 alike
+      const float m_new = mx > st.m + 8.f || st.m == -INFINITY ? fmaxf(st.m, mx) : st.m;
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[k], at.scale2, -ref));
+        sum += p[k];
+      }
+      if (__any(m_new != st.m)) {
+        const float alpha = __builtin_amdgcn_exp2f(st.m - ref);
+        st.l *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) st.o[e][k] *= alpha;
+      }
+      st.l += sum;
+      st.m = m_new;
+      // (what only some rows see is in V; a weight of zero does not silence infinities and NaN)
+      const bool odd = masked && b.p_lo != b.p_hi && (odd_at[cur][0] | odd_at[cur][1] | odd_at[cur][2] | odd_at[cur][3]);
+      u32x4 pw[4];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) pw[k >> 2][k & 3] = pack2(p[2 * k], p[2 * k + 1]);
+      if (odd) products_odd(Vs, pw, live, lane, st);
+      else products_v(Vs, pw, lane, st);
+    }
+    if (i + 1 < t_end) {
+      ok = ok_next;
+      masked = ok != 15 || !all_see(at, b, next * kStep, next * kStep + kStep - 1);
+      store_step<FOUR>(at, b, next, ok, masked, raw, lds + (cur ^ 1) * kStage, odd_at[cur ^ 1]);
+    }
+    __syncthreads();
+  }
+
+  // the rows, turned so that 16 lanes hold one
+  float* turn = reinterpret_cast<float*>(lds) + wave * 32 * kJoin;
+  float l = st.l;
+  l += __shfl_xor(l, 32);
+  const float m = part_max(st.m, l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+      *reinterpret_cast<f32x4*>(turn + n * kJoin + 32 * e + 8 * q4 + 4 * hh) =
+          f32x4{st.o[e][4 * q4], st.o[e][4 * q4 + 1], st.o[e][4 * q4 + 2], st.o[e][4 * q4 + 3]};
+  wave_sync();
+  const int piece = lane & 15;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int row = 4 * k + (lane >> 4), rr = w.r0 + row;
+    const float rm = __shfl(m, row), rl = __shfl(l, row);
+    if (rr >= b.n_rows) continue;
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = turn[row * kJoin + 8 * piece + e];
+    put_row(at, b.q0 + rr / at.group, h * at.group + rr % at.group, chunk, piece, o, rm, rl);
   }
 }
 
@@ -668,7 +983,7 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv,
 }
 
 template <class... A>
-hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t st, A... args) {
+hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t st, std::common_type_t<A>... args) {
   void* p[] = {(void*)&args...};
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)blocks), dim3((unsigned)threads), p, 0, st);
 }
@@ -685,9 +1000,14 @@ hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hip
 
 hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st) {
   const int64_t blocks = p.ids * kv.heads * p.n_chunks;
-  auto kernel = p.block_rows == 16 ? (four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>)
-                                   : (four ? tdk_kv_attend_rows_kernel<true, 2> : tdk_kv_attend_rows_kernel<false, 2>);
-  hipError_t e = launch(kernel, blocks, 256, st, kv, at);
+  hipError_t e;
+  if (p.block_rows == 128) {
+    e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at, (int)(p.ids - 1));
+  } else {
+    auto kernel = p.block_rows == 16 ? (four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>)
+                                     : (four ? tdk_kv_attend_rows_kernel<true, 2> : tdk_kv_attend_rows_kernel<false, 2>);
+    e = launch(kernel, blocks, 256, st, kv, at);
+  }
   if (e == hipSuccess && p.n_chunks > 1) e = launch(tdk_kv_attend_join_kernel, (p.rows + 15) / 16, 256, st, kv, at, p.rows);
   return e;
 }

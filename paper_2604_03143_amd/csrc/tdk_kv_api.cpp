@@ -58,7 +58,7 @@ KvDev kv_dev(const tdk_kv* kv, const tdk_kv_cache* c, const tdk_kv_batch* b) {
   KvDev d;
   d.k = static_cast<char*>(c->k);
   d.v = static_cast<char*>(c->v);
-  d.pool_pages = c->pool_pages;
+  d.pool_pages = (int32_t)c->pool_pages;
   d.q_start = b->q_start;
   d.seq_len = b->seq_len;
   d.table = b->block_table;
@@ -137,7 +137,7 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   if (b->n_seqs == 0 || b->n_tokens == 0) return true;
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_tokens * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
-  p.block_rows = per_seq <= 16 ? 16 : 32;
+  p.block_rows = per_seq <= 16 ? 16 : per_seq <= 64 ? 32 : 128;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // A sequence is cut where its row blocks alone leave compute units idle: two workgroups of four wavefronts each fit on one.
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
