@@ -54,7 +54,8 @@ struct KvAttendDev {
   int32_t        window, n_sink;
   int32_t        n_chunks;     // parts of the sequence that workgroups take apart
   int32_t        q_flip;       // the caller's scale was negative: the queries carry the sign
-  float          scale2;       // magnitude of the scale, times log2(e)
+  float          scale;        // its magnitude
+  float          scale2;       // times log2(e)
 };
 
 // How a call of the attention is cut.

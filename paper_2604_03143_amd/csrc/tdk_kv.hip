@@ -2,37 +2,19 @@
 // queries to the pages, and rows back out of them.
 #include "tdk_kv.h"
 #include "tdk_internal.h"
+#include "tdk_tiles.h"
 
 #include <type_traits>
 
 namespace tdk {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 namespace {
 
 constexpr int kRow = 2 * kHeadDim;         // bytes of a bf16 head row
 constexpr int kRow4 = kHeadDim / 2;        // bytes of its 4-bit values
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const f32x2 v = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-__device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// Orders the LDS traffic of one wavefront: no hardware barrier, only a point the compiler may not move memory accesses across.
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 // For i in [0, n), at(i) not decreasing: how many are <= x.  The lanes of a wavefront probe 64 places a round (one round up to
 // 64 entries, two up to 4096).  A round leaves less than a 64th of the range, whatever the values are.
@@ -247,10 +229,6 @@ __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const K
 // Attention.  The query rows of a sequence and KV head are its (token, head of the group) pairs, tokens first; a workgroup takes a
 // block of them and a part of the tokens they see.  Scores are kept in base 2: s = (q . k) scale log2(e).
 // ---------------------------------------------------------------------------------------------
-constexpr int kTile = 32;                  // tokens per step of a wavefront
-constexpr int kVsStride = kHeadDim + 32;   // bf16 elements per staged V row (+64 bytes: four rows' 64-byte pieces then lie in different
-                                           // LDS banks for the transposing reads)
-
 // A block of query rows: which sequence it belongs to, and what its rows see.
 struct Block {
   int s;              // sequence
@@ -329,13 +307,10 @@ __device__ __forceinline__ bool one_sees(const KvAttendDev& at, const Block& b, 
   return j <= b.p_hi && (at.window == 0 || b.p_lo - j < at.window || j < at.n_sink) && !(j >= b.hole_b && j < b.hole_e);
 }
 
-// Base 2 logarithm of a sum's scale joined with the sum: what the caller gets is the natural one.
-__device__ __forceinline__ float row_lse(float m2, float l) {
+// log-sum-exp of a row from its maximum in base 2: -infinity for an empty one, NaN for a row with a NaN score
+__device__ __forceinline__ float row_lse2(float m2, float l) {
   return l > 0.f ? 0.69314718055994531f * m2 + __logf(l) : l != l ? l : -INFINITY;
 }
-// The maximum that goes with a partial sum.  A NaN score leaves a row's reference point at -infinity, and joining takes that for an
-// empty part: such a part says +infinity instead, and the row becomes NaN.
-__device__ __forceinline__ float part_max(float m, float l) { return m == -INFINITY && l != l ? INFINITY : m; }
 
 // Eight elements of a finished row (un-normalised sums o, maximum m2, sum l): joined with the caller's partial result and written.
 __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int hq, int piece, const float (&o)[8], float m2, float l) {
@@ -343,7 +318,7 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
   float r[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = o[i] * inv;
-  float lse = row_lse(m2, l);
+  float lse = row_lse2(m2, l);
   const int64_t idx = tok * at.n_q_heads + hq;
   if (at.other_out) {
     const float pl = at.other_lse[idx];
@@ -679,121 +654,71 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ---------------------------------------------------------------------------------------------
-// Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS, two stages of them: the next step's
-// pages are on their way into registers while this one's products run, and go into the other stage behind them.
+// Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS (tdk_tiles.h): the score products of the next
+// step stand beside the weights and second products of this one, and the pages of the steps behind those travel to LDS meanwhile; 4-bit
+// pages by way of registers, where they become bf16.
 // ---------------------------------------------------------------------------------------------
-constexpr int kStep = 64;                  // tokens per step of a workgroup
-constexpr int kKsStride = kHeadDim + 8;    // bf16 elements per staged K row (+16 bytes: spreads LDS banks)
-constexpr int kStageK = kStep * kKsStride, kStage = kStageK + kStep * kVsStride;      // elements
+constexpr int kBlockRows = 4 * 32;
+constexpr float kLog2e = 1.4426950408889634f;
 
-// A step's K and V on their way: bf16: 16 bytes (thread % 16) of tokens 16 it + thread / 16; 4 bits: block thread % 4 of token thread / 4.
-template <bool FOUR>
-struct RawStep {
-  u32x4 k[FOUR ? 1 : 4], v[FOUR ? 1 : 4];
-  uint32_t ke, ve;
+struct StepShared {
+  unsigned char k[2][kStepTile];
+  unsigned char v[2][kStepTile];
+  int odd[4];
 };
 
-template <bool FOUR>
-__device__ __forceinline__ void load_step(const KvDev& kv, const Pages<4>& pg, int h, int wave, RawStep<FOUR>& r) {
-  const int tid = threadIdx.x, lane = tid & 63, T = 1 << kv.page_shift;
-  if constexpr (FOUR) {
-    const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
-    const int row0 = 16 * wave & (T - 1);
-    const int64_t base = (page * kv.heads + h) * (T * 68);
-    r.k[0] = *reinterpret_cast<const u32x4*>(kv.k + base + row0 * kRow4 + 16 * lane);
-    r.ke = *reinterpret_cast<const uint8_t*>(kv.k + base + (T * kRow4 + row0 * 4) + lane);
-    r.v[0] = *reinterpret_cast<const u32x4*>(kv.v + base + row0 * kRow4 + 16 * lane);
-    r.ve = *reinterpret_cast<const uint8_t*>(kv.v + base + (T * kRow4 + row0 * 4) + lane);
-  } else {
-    const int lane_off = (tid >> 4) * kv.heads * kRow + 16 * (tid & 15);
-#pragma unroll
-    for (int it = 0; it < 4; ++it) {
-      const int64_t base = ((((int64_t)max(pg.p[it], 0) << kv.page_shift) + (16 * it & (T - 1))) * kv.heads + h) * kRow;
-      r.k[it] = *reinterpret_cast<const u32x4*>(kv.k + base + lane_off);
-      r.v[it] = *reinterpret_cast<const u32x4*>(kv.v + base + lane_off);
-    }
-  }
-}
-
-// Into a stage.  masked: some row of the block does not see some token; then tokens that none sees become zeros in V, and the wavefront's entry
-// of `odd` says whether what is left holds infinities or NaN.
-template <bool FOUR>
-__device__ __forceinline__ void store_step(const KvAttendDev& at, const Block& b, int tile, int ok, bool masked, RawStep<FOUR>& r, uint16_t* stage, int* odd) {
-  const int tid = threadIdx.x;
-  bool strange = false;
-  if constexpr (FOUR) {
-    const int t = tid >> 2, c = 32 * (tid & 3);
-    if (masked) {
-      if (!((ok >> (t >> 4) & 1) && one_sees(at, b, tile * kStep + t))) { r.v[0] = u32x4{0, 0, 0, 0}; r.ve = 0; }
-      strange = r.ve == 255;
-    }
-    u32x4* dk = reinterpret_cast<u32x4*>(stage + t * kKsStride + c);
-    u32x4* dv = reinterpret_cast<u32x4*>(stage + kStageK + t * kVsStride + c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      dk[e] = from4(r.k[0][e], r.ke);
-      dv[e] = from4(r.v[0][e], r.ve);
-    }
-  } else {
-#pragma unroll
-    for (int it = 0; it < 4; ++it) {
-      const int t = 16 * it + (tid >> 4), c = 8 * (tid & 15);
-      if (masked) {
-        if (!((ok >> it & 1) && one_sees(at, b, tile * kStep + t))) r.v[it] = u32x4{0, 0, 0, 0};
-        strange |= odd16(r.v[it][0]) || odd16(r.v[it][1]) || odd16(r.v[it][2]) || odd16(r.v[it][3]);
-      }
-      *reinterpret_cast<u32x4*>(stage + t * kKsStride + c) = r.k[it];
-      *reinterpret_cast<u32x4*>(stage + kStageK + t * kVsStride + c) = r.v[it];
-    }
-  }
-  if (masked) {
-    const int any = __any(strange);
-    if ((tid & 63) == 0) odd[tid >> 6] = any;
-  }
-}
-
-// Running softmax of 32 query rows: lane (n, hh) = (lane % 32, lane / 32) holds row n, elements 32 b + 8 (i / 4) + 4 hh + i % 4 of it.
-struct Rows32 {
-  float m, l;
-  f32x16 o[4];
-};
-
-// O^T += V^T P^T for a step.  p[i]: the weight of token 32 (i / 16) + 8 ((i % 16) / 4) + 4 hh + i % 4.  Within 16 lanes a transposing read takes
-// the lanes' 8-byte pieces as the rows of a 16 x 4 matrix and hands lane i its column: with lane i at (token i / 4, four elements i % 4) it
-// gets element i of the four tokens.
-__device__ __forceinline__ u32x4 operand_v(const uint16_t* Vs, int kk, int e, int lane) {
-  const int i16 = lane & 15, blk = lane >> 4;
-  const uint16_t* at = Vs + (4 * (blk >> 1) + (i16 >> 2)) * kVsStride + 16 * (blk & 1) + 4 * (i16 & 3) + 16 * kk * kVsStride + 32 * e;
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * kVsStride));
-  const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-  return u32x4{l2.x, l2.y, h2.x, h2.y};
-}
-__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ void products_v(const uint16_t* Vs, const u32x4 (&pw)[4], int lane, Rows32& st) {
-#pragma unroll
-  for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) st.o[e] = mfma32(operand_v(Vs, kk, e, lane), pw[kk], st.o[e]);
-}
-// The same where V holds what only some of the rows may meet (kind_of); bit i of live: the row sees token i of the lane's 32.
-__device__ __forceinline__ void products_odd(const uint16_t* Vs, const u32x4 (&pw)[4], uint32_t live, int lane, Rows32& st) {
+// One plane's 64 tokens of a step: bf16 straight into the LDS tile.  Page groups: 16 tokens, one of the four parts of the tile each.  A page that
+// is not there: page 0 is read in its place and what it holds is not seen.
+__device__ __forceinline__ void fetch_step(const KvDev& kv, const char* plane, const Pages<4>& pg, int h, const StepLoader& ld, uint32_t off, uint32_t lds) {
+  const int T = 1 << kv.page_shift;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
+    const int64_t row = ((int64_t)max(pg.p[e], 0) << kv.page_shift) + (16 * e & (T - 1));
+    load_to_lds(plane + (row * kv.heads + h) * kRow, off, lds + 4096u * e + ld.lds_wave);
+  }
+}
+
+// 4 bits: lane l of wavefront w holds block l % 4 of token 16 w + l / 4.
+struct Codes {
+  u32x4 c;
+  uint32_t e;
+};
+__device__ __forceinline__ Codes fetch_codes(const KvDev& kv, const char* plane, const Pages<4>& pg, int h, int wave, int lane) {
+  const int T = 1 << kv.page_shift;
+  const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
+  const int row0 = 16 * wave & (T - 1);
+  const char* base = plane + (page * kv.heads + h) * (T * 68);
+  return Codes{*reinterpret_cast<const u32x4*>(base + row0 * kRow4 + 16 * lane), *reinterpret_cast<const uint8_t*>(base + (T * kRow4 + row0 * 4) + lane)};
+}
+template <bool V>
+__device__ __forceinline__ void put_codes(const Codes& x, unsigned char* tile, int wave, int lane) {
+  const int t = 16 * wave + (lane >> 2);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) st.o[e] = mfma32(kind_of(operand_v(Vs, kk, e, lane), 0), pw[kk], st.o[e]);
+  for (int e = 0; e < 4; ++e) {
+    const int c = 4 * (lane & 3) + e;
+    *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from4(x.c[e], x.e);
+  }
+}
+
+// A step whose V holds what only some rows may meet: infinity or NaN goes to the sums of the rows that see its token (kind_of), before the step
+// itself takes the finite part.  live: bit i: the row sees token 32 (i / 16) + 8 ((i % 16) / 4) + 4 hh + i % 4.
+__device__ __forceinline__ void add_odd(const unsigned char* Vs, uint32_t live, int lane, RowState& st) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+#pragma clang loop unroll(disable)
     for (int kind = 1; kind <= 3; ++kind) {
       f32x16 hit;
 #pragma unroll
       for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma clang loop unroll(disable)
       for (int kk = 0; kk < 4; ++kk) {
         const uint32_t l8 = live >> (8 * kk);
-        hit = mfma32(kind_of(operand_v(Vs, kk, e, lane), kind), u32x4{ones(l8, 0), ones(l8, 1), ones(l8, 2), ones(l8, 3)}, hit);
+        const u32x4 see = {ones(l8, 0), ones(l8, 1), ones(l8, 2), ones(l8, 3)};
+        const u32x4 v = kind_of(__builtin_bit_cast(u32x4, v_operand(Vs, kk, q, lane)), kind);
+        hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, see), hit, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) st.o[e][i] += hit[i] > 0.f ? value_of(kind) : 0.f;
+      for (int i = 0; i < 16; ++i) st.oacc[q][i] += hit[i] > 0.f ? value_of(kind) : 0.f;
     }
   }
 }
@@ -801,22 +726,19 @@ __device__ __forceinline__ void products_odd(const uint16_t* Vs, const u32x4 (&p
 template <bool FOUR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_tile_kernel(const KvDev kv, const KvAttendDev at,
                                                                                                             const int last_id) {
-  constexpr int kJoin = kHeadDim + 4;        // floats per row of the area that turns the results
-  __shared__ __align__(16) uint16_t lds[2 * kStage];
-  __shared__ int odd_at[2][4];
-  static_assert(4 * 32 * kJoin * 4 <= 2 * kStage * 2, "the turning area lies over the stages");
+  __shared__ __align__(16) StepShared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hh = lane >> 5;
   const int h = blockIdx.x % kv.heads;
   const int rest = blockIdx.x / kv.heads, chunk = rest % at.n_chunks;
   Block b;
   // (a causal prompt's last rows see most: they start first)
-  if (!find_block(kv, at, last_id - rest / at.n_chunks, 128, lane, b)) return;
-  const Tiles tiles = tiles_of(kv, at, b, kStep);
+  if (!find_block(kv, at, last_id - rest / at.n_chunks, kBlockRows, lane, b)) return;
+  const Tiles tiles = tiles_of(kv, at, b, kBigTile);
   const int t_begin = (int)((int64_t)tiles.total * chunk / at.n_chunks), t_end = (int)((int64_t)tiles.total * (chunk + 1) / at.n_chunks);
   // the wavefront's own rows
   Block w = b;
   w.r0 = b.r0 + 32 * wave;
-  const bool any_row = w.r0 < b.n_rows;
+  const bool active = w.r0 < b.n_rows;
   w.p_lo = b.pos0 + w.r0 / at.group;
   w.p_hi = b.pos0 + (min(w.r0 + 32, b.n_rows) - 1) / at.group;
 
@@ -835,116 +757,127 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       qf[kk] = __builtin_bit_cast(bf16x8, x);
     }
   }
-  Rows32 st;
-  st.m = -INFINITY;
-  st.l = 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) st.o[e][i] = 0.f;
+  RowState st;
+  row_state_init(st);
+  const StepLoader ld(kv.heads);
+  const uint32_t lds_k[2] = {lds_byte(sh.k[0]), lds_byte(sh.k[1])}, lds_v[2] = {lds_byte(sh.v[0]), lds_byte(sh.v[1])};
 
-  RawStep<FOUR> raw;
-  Pages<4> pages{};
-  int ok = 0;
-  bool masked = false;
-  if (t_begin < t_end) {
-    const int tile = tiles.tile(t_begin);
-    pages = pages_of<4>(kv, b.s, tile);
-    ok = there(pages);
-    load_step<FOUR>(kv, pages, h, wave, raw);
-    if (t_begin + 1 < t_end) pages = pages_of<4>(kv, b.s, tiles.tile(t_begin + 1));
-    masked = ok != 15 || !all_see(at, b, tile * kStep, tile * kStep + kStep - 1);
-    store_step<FOUR>(at, b, tile, ok, masked, raw, lds, odd_at[0]);
-  }
-  __syncthreads();
-  for (int i = t_begin; i < t_end; ++i) {
-    const int cur = (i - t_begin) & 1;
-    const int tile = tiles.tile(i), j0 = tile * kStep;
-    const int next = i + 1 < t_end ? tiles.tile(i + 1) : 0;
-    const int ok_next = there(pages);
-    if (i + 1 < t_end) load_step<FOUR>(kv, pages, h, wave, raw);
-    if (i + 2 < t_end) pages = pages_of<4>(kv, b.s, tiles.tile(i + 2));
-    const uint16_t* Ks = lds + cur * kStage;
-    const uint16_t* Vs = Ks + kStageK;
-    // (does some row of the wavefront see some token of the step?)
-    const bool some = any_row && j0 <= w.p_hi && (at.window == 0 || w.p_lo - (j0 + kStep - 1) < at.window || j0 < at.n_sink);
-    if (some) {
-      f32x16 s[2];
+  // The tokens of a step that the lane's row sees.  kinds: which tests the step needs (first bit: the end, second: window, third: hole or pages)
+  const auto live_of = [&](int j0, int ok) __attribute__((always_inline)) {
+    const int a = pos - j0 - 4 * hh, sink = at.n_sink - j0 - 4 * hh, hb = b.hole_b - j0 - 4 * hh, he = b.hole_e - j0 - 4 * hh;
+    uint32_t live = 0;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          const u32x4 a = *reinterpret_cast<const u32x4*>(Ks + (32 * tt + n) * kKsStride + 16 * kk + 8 * hh);
-          s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qf[kk], s[tt], 0, 0, 0);
-        }
-      float p[32];
-#pragma unroll
-      for (int k = 0; k < 32; ++k) p[k] = s[k >> 4][k & 15];
-      const bool own_mask = masked && (ok != 15 || !all_see(at, w, j0, j0 + kStep - 1));
-      uint32_t live = ~0u;
-      if (own_mask) {
-        const int a = pos - j0 - 4 * hh, lo = at.window ? a - at.window : -1, sink = at.n_sink - j0 - 4 * hh;
-        const int hb = b.hole_b - j0 - 4 * hh, he = b.hole_e - j0 - 4 * hh;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const int t = 32 * (k >> 4) + 8 * ((k & 15) >> 2) + (k & 3);
-          const bool see = t <= a && (at.window == 0 || t > lo || t < sink) && !(t >= hb && t < he) && (ok >> (t >> 4) & 1);
-          p[k] = see ? p[k] : -INFINITY;
-          live = see ? live : live & ~(1u << k);
-        }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(p[k], p[k + 1]));
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * at.scale2;
-      // the reference point moves only where a score passes it by 2^8: until then the weights are at most that, in fp32 and bf16 alike
-      const float m_new = mx > st.m + 8.f || st.m == -INFINITY ? fmaxf(st.m, mx) : st.m;
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
-      float sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[k], at.scale2, -ref));
-        sum += p[k];
-      }
-      if (__any(m_new != st.m)) {
-        const float alpha = __builtin_amdgcn_exp2f(st.m - ref);
-        st.l *= alpha;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int k = 0; k < 16; ++k) st.o[e][k] *= alpha;
-      }
-      st.l += sum;
-      st.m = m_new;
-      // (what only some rows see is in V; a weight of zero does not silence infinities and NaN)
-      const bool odd = masked && b.p_lo != b.p_hi && (odd_at[cur][0] | odd_at[cur][1] | odd_at[cur][2] | odd_at[cur][3]);
-      u32x4 pw[4];
-#pragma unroll
-      for (int k = 0; k < 16; ++k) pw[k >> 2][k & 3] = pack2(p[2 * k], p[2 * k + 1]);
-      if (odd) products_odd(Vs, pw, live, lane, st);
-      else products_v(Vs, pw, lane, st);
+    for (int k = 0; k < 32; ++k) {
+      const int t = 32 * (k >> 4) + 8 * ((k & 15) >> 2) + (k & 3);
+      if (t <= a && (at.window == 0 || a - t < at.window || t < sink) && !(t >= hb && t < he) && (ok >> (t >> 4) & 1)) live |= 1u << k;
     }
-    if (i + 1 < t_end) {
-      ok = ok_next;
-      masked = ok != 15 || !all_see(at, b, next * kStep, next * kStep + kStep - 1);
-      store_step<FOUR>(at, b, next, ok, masked, raw, lds + (cur ^ 1) * kStage, odd_at[cur ^ 1]);
+    return live;
+  };
+  const auto mask_scores = [&](int j0, int ok, f32x16 (&s)[2], float& mx) __attribute__((always_inline)) {
+    if (ok == 15 && all_see(at, w, j0, j0 + kBigTile - 1)) return;
+    const uint32_t live = live_of(j0, ok);
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (!(live >> k & 1)) s[k >> 4][k & 15] = -INFINITY;
+    rows_max<2>(s, mx);
+  };
+
+  if (t_begin < t_end) {
+    f32x16 s0[2], s1[2];
+    Pages<4> here = pages_of<4>(kv, b.s, tiles.tile(t_begin)), next = here, after = here;
+    if (t_begin + 1 < t_end) next = pages_of<4>(kv, b.s, tiles.tile(t_begin + 1));
+    if (t_begin + 2 < t_end) after = pages_of<4>(kv, b.s, tiles.tile(t_begin + 2));
+    if constexpr (FOUR) {
+      const Codes k0 = fetch_codes(kv, kv.k, here, h, wave, lane), v0 = fetch_codes(kv, kv.v, here, h, wave, lane), k1 = fetch_codes(kv, kv.k, next, h, wave, lane);
+      put_codes<false>(k0, sh.k[0], wave, lane);
+      put_codes<true>(v0, sh.v[0], wave, lane);
+      put_codes<false>(k1, sh.k[1], wave, lane);
+    } else {
+      fetch_step(kv, kv.k, here, h, ld, ld.k_off, lds_k[0]);
+      fetch_step(kv, kv.v, here, h, ld, ld.v_off, lds_v[0]);
+      fetch_step(kv, kv.k, next, h, ld, ld.k_off, lds_k[1]);
+      landed();
     }
     __syncthreads();
+    if (active) {
+      float mx;
+      rows_scores(sh.k[0], qf, n, hh, s0);
+      rows_max<2>(s0, mx);
+      mask_scores(tiles.tile(t_begin) * kBigTile, there(here), s0, mx);
+      rows_settle(mx, at.scale, st);
+    }
+    __syncthreads();                         // the first step replaces its K tile
+    int i = t_begin;
+    const auto step = [&](int odd, f32x16 (&s)[2], f32x16 (&nx)[2]) __attribute__((always_inline)) {
+      const int j0 = tiles.tile(i) * kBigTile, ok = there(here);
+      // V of a step that some rows see and some do not: what none sees becomes zero where it lies (a weight of zero would not silence infinity
+      // or NaN); if what is left is not finite, the rows that see it have it now, and the step meets the finite part
+      if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
+        u32x4* own = reinterpret_cast<u32x4*>(sh.v[odd] + 16 * threadIdx.x);
+        bool mine = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const u32x4 x = own[256 * e];
+          if (!((ok >> e & 1) && one_sees(at, b, j0 + 16 * e + (int)(threadIdx.x >> 4)))) own[256 * e] = u32x4{0, 0, 0, 0};
+          else mine |= odd16(x[0]) || odd16(x[1]) || odd16(x[2]) || odd16(x[3]);
+        }
+        const int any = __any(mine);
+        if (lane == 0) sh.odd[wave] = any;
+        __syncthreads();
+        if (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) {
+          if (active) add_odd(sh.v[odd], live_of(j0, ok), lane, st);
+          __syncthreads();
+#pragma unroll
+          for (int e = 0; e < 4; ++e) own[256 * e] = kind_of(own[256 * e], 0);
+          __syncthreads();
+        }
+      }
+      Codes ck, cv;
+      if constexpr (FOUR) {                  // (nobody reads these two tiles in this step)
+        ck = fetch_codes(kv, kv.k, after, h, wave, lane);
+        cv = fetch_codes(kv, kv.v, next, h, wave, lane);
+      } else {
+        fetch_step(kv, kv.k, after, h, ld, ld.k_off, lds_k[odd]);
+        fetch_step(kv, kv.v, next, h, ld, ld.v_off, lds_v[odd ^ 1]);
+      }
+      here = next;
+      next = after;
+      if (i + 3 < t_end) after = pages_of<4>(kv, b.s, tiles.tile(i + 3));
+      if (active) {
+        float mx;
+        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, lane, st);      // (past the last step: scores that are not used)
+        if (i + 1 < t_end) {
+          mask_scores(tiles.tile(i + 1) * kBigTile, there(here), nx, mx);
+          rows_settle(mx, at.scale, st);
+        }
+      }
+      if constexpr (FOUR) {
+        put_codes<false>(ck, sh.k[odd], wave, lane);
+        put_codes<true>(cv, sh.v[odd ^ 1], wave, lane);
+      } else {
+        landed();
+      }
+      __syncthreads();
+      ++i;
+    };
+    while (i < t_end) {
+      step(0, s0, s1);
+      if (i < t_end) step(1, s1, s0);
+    }
   }
 
-  // the rows, turned so that 16 lanes hold one
-  float* turn = reinterpret_cast<float*>(lds) + wave * 32 * kJoin;
-  float l = st.l;
+  // The rows go out by way of LDS, where 16 lanes hold one: piece c (16 bytes) of row n stands at place c ^ n.
+  char* turn = reinterpret_cast<char*>(&sh) + wave * 32 * 4 * kHeadDim;
+  static_assert(4 * 32 * 4 * kHeadDim <= 2 * sizeof(StepShared::k), "a wavefront's rows lie over the tiles");
+  float l = st.l_run;
   l += __shfl_xor(l, 32);
-  const float m = part_max(st.m, l);
+  const float m = part_max(st.m_run, l) * kLog2e;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4)
-      *reinterpret_cast<f32x4*>(turn + n * kJoin + 32 * e + 8 * q4 + 4 * hh) =
-          f32x4{st.o[e][4 * q4], st.o[e][4 * q4 + 1], st.o[e][4 * q4 + 2], st.o[e][4 * q4 + 3]};
+      *reinterpret_cast<f32x4*>(turn + n * 512 + 16 * ((8 * e + 2 * q4 + hh) ^ n)) =
+          f32x4{st.oacc[e][4 * q4], st.oacc[e][4 * q4 + 1], st.oacc[e][4 * q4 + 2], st.oacc[e][4 * q4 + 3]};
   wave_sync();
   const int piece = lane & 15;
 #pragma unroll
@@ -952,9 +885,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int row = 4 * k + (lane >> 4), rr = w.r0 + row;
     const float rm = __shfl(m, row), rl = __shfl(l, row);
     if (rr >= b.n_rows) continue;
-    float o[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = turn[row * kJoin + 8 * piece + e];
+    const f32x4 x = *reinterpret_cast<const f32x4*>(turn + row * 512 + 16 * ((2 * piece) ^ row));
+    const f32x4 y = *reinterpret_cast<const f32x4*>(turn + row * 512 + 16 * ((2 * piece + 1) ^ row));
+    const float o[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     put_row(at, b.q0 + rr / at.group, h * at.group + rr % at.group, chunk, piece, o, rm, rl);
   }
 }
