@@ -52,7 +52,9 @@ struct KvAttendDev {
   int32_t        n_q_heads;
   int32_t        group;        // query heads per KV head
   int32_t        window, n_sink;
-  int32_t        n_chunks;     // parts of the sequence that workgroups take apart
+  int32_t        n_chunks;     // parts of a sequence at most, each a workgroup's
+  int32_t        piece_tiles;  // tiles of a part
+  int32_t        n_rest;       // row blocks times parts
   int32_t        q_flip;       // the caller's scale was negative: the queries carry the sign
   float          scale;        // its magnitude
   float          scale2;       // times log2(e)
@@ -63,6 +65,7 @@ struct KvAttendPlan {
   int32_t block_rows = 16;     // query rows (token, head of the group) per workgroup
   int64_t ids = 0;             // row blocks: an upper bound over all ways the tokens can be spread over the sequences
   int32_t n_chunks = 1;
+  int32_t piece_tiles = 1;
   int64_t rows = 0;            // n_tokens * n_q_heads
   size_t  o_part_ml = 0, bytes = 0;
 };

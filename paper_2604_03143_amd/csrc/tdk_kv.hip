@@ -16,6 +16,10 @@ namespace {
 constexpr int kRow = 2 * kHeadDim;         // bytes of a bf16 head row
 constexpr int kRow4 = kHeadDim / 2;        // bytes of its 4-bit values
 
+// A load that passes the caches by, for what is read once.
+template <class T>
+__device__ __forceinline__ T load_once(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(p)); }
+
 // For i in [0, n), at(i) not decreasing: how many are <= x.  The lanes of a wavefront probe 64 places a round (one round up to
 // 64 entries, two up to 4096).  A round leaves less than a 64th of the range, whatever the values are.
 template <class F>
@@ -240,17 +244,23 @@ struct Block {
   int hole_b, hole_e;
 };
 
-// Row blocks are numbered without knowing the lengths: sequence s starts at number floor(q0 group / block) + s, which leaves at least
-// as many numbers as it has blocks.  False: no block has this number.
+// Row blocks are numbered without knowing the lengths: number s is the first block of sequence s; behind those, sequence s has the numbers
+// from floor(q0 group / block) on, at least as many as it has further blocks.  (One token per sequence: no number without a block in between, and
+// nothing to search.)  False: no block has this number.
 __device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& at, int id, int block_rows, int lane, Block& b) {
-  const auto first = [&](int i) { return (int64_t)start_of(kv, i) * at.group / block_rows + i; };
-  b.s = count_up_to(first, kv.n_seqs, id, lane) - 1;
-  if (b.s < 0) return false;
+  int64_t r0 = 0;
+  if (id < kv.n_seqs) {
+    b.s = id;
+  } else {
+    const int e = id - kv.n_seqs;
+    b.s = count_up_to([&](int i) { return (int64_t)start_of(kv, i) * at.group / block_rows; }, kv.n_seqs, e, lane) - 1;
+    if (b.s < 0) return false;
+    r0 = (e - (int64_t)start_of(kv, b.s) * at.group / block_rows + 1) * block_rows;
+  }
   b.q0 = min(max(scalar_read(kv.q_start + b.s), 0), kv.n_tokens);
   const int n = min(max(scalar_read(kv.q_start + b.s + 1), 0), kv.n_tokens) - b.q0;
   if (n <= 0) return false;
   b.n_rows = n * at.group;                   // (at most n_tokens * n_q_heads, which the host has checked)
-  const int64_t r0 = (id - first(b.s)) * block_rows;
   if (r0 >= b.n_rows) return false;
   b.r0 = (int)r0;
   b.pos0 = max(scalar_read(kv.seq_len + b.s), 0) - n;      // (tokens of a call and of a table are at most 2^30: differences of positions fit)
@@ -294,6 +304,13 @@ __device__ __forceinline__ Tiles tiles_of(const KvDev& kv, const KvAttendDev& at
     t.total += t.count[k];
   }
   return t;
+}
+
+// A workgroup's part of the tiles: pieces of one length, so that long sequences have many and short ones few; the last takes what is left of
+// a sequence longer than expected.
+__device__ __forceinline__ void part_of(const KvAttendDev& at, const Tiles& t, int chunk, int& begin, int& end) {
+  begin = (int)min((int64_t)chunk * at.piece_tiles, (int64_t)t.total);
+  end = chunk == at.n_chunks - 1 ? t.total : min(begin + at.piece_tiles, t.total);
 }
 
 __device__ __forceinline__ bool sees(const KvAttendDev& at, const Block& b, int p, int j) {
@@ -351,6 +368,14 @@ __device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int 
   if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{m2, l};
 }
 
+// A part with no tokens: nothing but that is kept of it.
+__device__ __forceinline__ void put_empty(const KvAttendDev& at, const Block& b, int h, int chunk, int block_rows) {
+  const int r = b.r0 + (int)threadIdx.x;
+  if ((int)threadIdx.x >= block_rows || r >= b.n_rows) return;
+  const int64_t row = (int64_t)(b.q0 + r / at.group) * at.n_q_heads + h * at.group + r % at.group;
+  *reinterpret_cast<f32x2*>(at.part_ml + 2 * (row * at.n_chunks + chunk)) = f32x2{-INFINITY, 0.f};
+}
+
 // Physical pages of the 16-token groups of a tile, -1 where there is none.  What follows is the same for the whole wavefront: scalar reads.
 template <int N>
 struct Pages { int p[N]; };
@@ -397,18 +422,18 @@ __device__ __forceinline__ void load_tile(const KvDev& kv, const Pages<2>& pg, i
       const int64_t base = (page * kv.heads + h) * (T * 68);
       const char* k = kv.k + base;
       const char* v = kv.v + base;
-      r.k[tt] = *reinterpret_cast<const u32x4*>(k + row0 * kRow4 + (n * kRow4 + 16 * g));
-      r.ke[tt] = *reinterpret_cast<const uint8_t*>(k + (T * kRow4 + row0 * 4) + (n * 4 + g));
-      r.v[tt] = *reinterpret_cast<const u32x4*>(v + row0 * kRow4 + 16 * lane);
-      r.ve[tt] = *reinterpret_cast<const uint8_t*>(v + (T * kRow4 + row0 * 4) + lane);
+      r.k[tt] = load_once<u32x4>(k + row0 * kRow4 + (n * kRow4 + 16 * g));
+      r.ke[tt] = load_once<uint8_t>(k + (T * kRow4 + row0 * 4) + (n * 4 + g));
+      r.v[tt] = load_once<u32x4>(v + row0 * kRow4 + 16 * lane);
+      r.ve[tt] = load_once<uint8_t>(v + (T * kRow4 + row0 * 4) + lane);
     } else {
       const int64_t base = (((page << kv.page_shift) + row0) * kv.heads + h) * kRow;
       const char* k = kv.k + base + (n * kv.heads * kRow + 16 * g);
       const char* v = kv.v + base + (g * kv.heads * kRow + 16 * n);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) r.k[2 * kk + tt] = *reinterpret_cast<const u32x4*>(k + 64 * kk);
+      for (int kk = 0; kk < 4; ++kk) r.k[2 * kk + tt] = load_once<u32x4>(k + 64 * kk);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.v[4 * tt + i] = *reinterpret_cast<const u32x4*>(v + 4 * i * kv.heads * kRow);
+      for (int i = 0; i < 4; ++i) r.v[4 * tt + i] = load_once<u32x4>(v + 4 * i * kv.heads * kRow);
     }
   }
 }
@@ -473,22 +498,51 @@ __device__ __forceinline__ float value_of(int kind) { return kind == 1 ? INFINIT
 // ones for the tokens 2 e, 2 e + 1 of a lane that its row sees
 __device__ __forceinline__ uint32_t ones(uint32_t live, int e) { return (live >> (2 * e) & 1u ? kOne : 0u) | (live >> (2 * e + 1) & 1u ? kOne << 16 : 0u); }
 
+// Which row block and part a workgroup takes (`rest`), and which KV head.  Workgroup i runs on XCD i % 8.
+//   The numbers of the row blocks have gaps, often regular ones: within each eight of them the places shift by one, so that no XCD gets the
+//   gaps alone.
+//   bf16: the heads of a row block go to different XCDs, and (by the caller, who adds the sequence and the part) a head to all of them in turn: a
+//   head's rows are 256 bytes apart by 256 H, and an XCD that reads one head only asks a part of the memory channels for everything (256
+//   sequences of 4000 tokens, 8 heads: 5.6 -> 5.9 TB/s, 64 of 16000 5.0 -> 5.7).
+//   4 bits: a head's part of a page is 1088 bytes, so neighbours share cache lines: all heads of a row block go to one XCD (4.9 -> 5.2 TB/s).
+template <bool TOGETHER>
+__device__ __forceinline__ int rest_of(int heads, int& h) {
+  int k;                                     // number before the shift
+  if (TOGETHER) {
+    const int turn = blockIdx.x >> 3;
+    h = turn % heads;
+    k = (blockIdx.x & 7) + 8 * (turn / heads);
+  } else {
+    h = blockIdx.x % heads;
+    k = blockIdx.x / heads;
+  }
+  return (k & ~7) | ((k + (k >> 3)) & 7);
+}
+
 // Few query rows (decoding, drafted tokens): a wavefront holds NR tiles of 16 rows and takes every fourth 32-token tile of the workgroup's
 // part; the four join at the end.  K goes from memory into the operands of the products as it lies there (S^T = K Q^T: lane (n, g) then
 // holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.
 template <bool FOUR, int NR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR == 1 ? 3 : 2, FOUR && NR == 1 ? 3 : 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
   constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
   __shared__ __align__(16) char lds[4 * kTile * kVsStride * 2];
   __shared__ float ml[4][16][2];
   static_assert(4 * 16 * kJoin * 4 <= 4 * kTile * kVsStride * 2, "the joining area lies over the V tiles");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % kv.heads;
-  const int rest = blockIdx.x / kv.heads, chunk = rest % at.n_chunks, id = rest / at.n_chunks;
+  int h;
+  const int rest = rest_of<FOUR>(kv.heads, h);
+  if (rest >= at.n_rest) return;
+  const int chunk = rest % at.n_chunks, id = rest / at.n_chunks;
   Block b;
   if (!find_block(kv, at, id, 16 * NR, lane, b)) return;
+  if constexpr (!FOUR) h = (h + b.s + chunk) % kv.heads;
   const Tiles tiles = tiles_of(kv, at, b, kTile);
-  const int t_begin = (int)((int64_t)tiles.total * chunk / at.n_chunks), t_end = (int)((int64_t)tiles.total * (chunk + 1) / at.n_chunks);
+  int t_begin, t_end;
+  part_of(at, tiles, chunk, t_begin, t_end);
+  if (t_begin == t_end && at.n_chunks > 1) {
+    put_empty(at, b, h, chunk, 16 * NR);
+    return;
+  }
 
   bf16x8 qf[NR][4];
   int pos[NR];
@@ -517,18 +571,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 
   uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kVsStride;
-  Raw<FOUR> next;
+  // Two tiles take turns: once the scores of one are there its registers belong to the tile after the next, which travels while this one's
+  // weights and second products run and the other tile is worked on.
+  Raw<FOUR> even, odds;
   Pages<2> pages{};
-  if (t_begin + wave < t_end) {
-    load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(t_begin + wave)), h, lane, next);
-    if (t_begin + wave + 4 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(t_begin + wave + 4));
-  }
-  for (int i = t_begin + wave; i < t_end; i += 4) {
-    Raw<FOUR> cur = next;
-    const int tile = tiles.tile(i), j0 = tile * kTile;
-    if (i + 4 < t_end) load_tile<FOUR>(kv, pages, h, lane, next);
-    if (i + 8 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(i + 8));
-    const bool masked = cur.ok != 3 || !all_see(at, b, j0, j0 + kTile - 1);
+  const int first = t_begin + wave;
+  if (first < t_end) load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(first)), h, lane, even);
+  if (first + 4 < t_end) load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(first + 4)), h, lane, odds);
+  if (first + 8 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(first + 8));
+  const auto step = [&](const int i, Raw<FOUR>& cur) __attribute__((always_inline)) {
+    const int tile = tiles.tile(i), j0 = tile * kTile, ok = cur.ok;
+    const bool masked = ok != 3 || !all_see(at, b, j0, j0 + kTile - 1);
     wave_sync();
     const bool odd = stage_v<FOUR>(at, b, tile, masked, lane, cur, Vs);
     wave_sync();
@@ -546,6 +599,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int rt = 0; rt < NR; ++rt)
           s[rt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[rt][kk], s[rt][tt], 0, 0, 0);
       }
+    if (i + 8 < t_end) load_tile<FOUR>(kv, pages, h, lane, cur);
+    if (i + 12 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(i + 12));
     bf16x8 pb[NR];
     uint32_t live[NR];
 #pragma unroll
@@ -555,7 +610,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         live[rt] = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if ((cur.ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live[rt] |= 1u << k;
+          if ((ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live[rt] |= 1u << k;
       }
       float p[8], mx = -INFINITY;
 #pragma unroll
@@ -594,29 +649,39 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
       return u32x4{l2.x, l2.y, h2.x, h2.y};
     };
-    if (!odd) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const u32x4 a = operand(e);
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt)
-          st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
-      }
-      continue;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
+    if (odd) {                               // what is not finite goes to the rows that see it, and the products meet the rest
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) {
-        st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kind_of(operand(e), 0)), pb[rt], st[rt].o[e], 0, 0, 0);
         const u32x4 see = {ones(live[rt], 0), ones(live[rt], 1), ones(live[rt], 2), ones(live[rt], 3)};
-        for (int kind = 1; kind <= 3; ++kind) {
-          const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kind_of(operand(e), kind)),
-                                                                     __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) st[rt].o[e][i] += hit[i] > 0.f ? value_of(kind) : 0.f;
-        }
+        for (int e = 0; e < 8; ++e)
+#pragma clang loop unroll(disable)
+          for (int kind = 1; kind <= 3; ++kind) {
+            const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kind_of(operand(e), kind)),
+                                                                       __builtin_bit_cast(bf16x8, see), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) st[rt].o[e][k] += hit[k] > 0.f ? value_of(kind) : 0.f;
+          }
       }
+      wave_sync();
+#pragma clang loop unroll(disable)
+      for (int k = 0; k < 8; ++k) {
+        u32x4* x = reinterpret_cast<u32x4*>(Vs + (4 * k + (lane >> 4)) * kVsStride + 8 * (lane & 15));
+        *x = kind_of(*x, 0);
+      }
+      wave_sync();
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const u32x4 a = operand(e);
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt)
+        st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
+    }
+  };
+  for (int i = first; i < t_end; i += 8) {
+    step(i, even);
+    if (i + 4 < t_end) step(i + 4, odds);
   }
 
   // the four wavefronts' rows joined: 16 lanes per row, eight elements each
@@ -728,13 +793,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                                                                                             const int last_id) {
   __shared__ __align__(16) StepShared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hh = lane >> 5;
-  const int h = blockIdx.x % kv.heads;
-  const int rest = blockIdx.x / kv.heads, chunk = rest % at.n_chunks;
+  int h;
+  const int rest = rest_of<false>(kv.heads, h), chunk = rest % at.n_chunks;
+  if (rest >= at.n_rest) return;
   Block b;
   // (a causal prompt's last rows see most: they start first)
   if (!find_block(kv, at, last_id - rest / at.n_chunks, kBlockRows, lane, b)) return;
+  h = (h + b.s + chunk) % kv.heads;
   const Tiles tiles = tiles_of(kv, at, b, kBigTile);
-  const int t_begin = (int)((int64_t)tiles.total * chunk / at.n_chunks), t_end = (int)((int64_t)tiles.total * (chunk + 1) / at.n_chunks);
+  int t_begin, t_end;
+  part_of(at, tiles, chunk, t_begin, t_end);
+  if (t_begin == t_end && at.n_chunks > 1) {
+    put_empty(at, b, h, chunk, kBlockRows);
+    return;
+  }
   // the wavefront's own rows
   Block w = b;
   w.r0 = b.r0 + 32 * wave;
@@ -782,17 +854,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     rows_max<2>(s, mx);
   };
 
+  constexpr int kPages = FOUR ? 5 : 3;
   if (t_begin < t_end) {
     f32x16 s0[2], s1[2];
-    Pages<4> here = pages_of<4>(kv, b.s, tiles.tile(t_begin)), next = here, after = here;
-    if (t_begin + 1 < t_end) next = pages_of<4>(kv, b.s, tiles.tile(t_begin + 1));
-    if (t_begin + 2 < t_end) after = pages_of<4>(kv, b.s, tiles.tile(t_begin + 2));
+    // Pages of this step and the next ones.  (Behind the last step the last one's are read again: what that gives is not used.)
+    Pages<4> ahead[5];
+#pragma unroll
+    for (int d = 0; d < 5; ++d) ahead[d] = d < kPages ? pages_of<4>(kv, b.s, tiles.tile(min(t_begin + d, t_end - 1))) : Pages<4>{};
+    Codes ck[2], cv[2];                      // 4 bits: K of the step behind the next and V of the next one, and both of the step after
     if constexpr (FOUR) {
-      const Codes k0 = fetch_codes(kv, kv.k, here, h, wave, lane), v0 = fetch_codes(kv, kv.v, here, h, wave, lane), k1 = fetch_codes(kv, kv.k, next, h, wave, lane);
+      const Codes k0 = fetch_codes(kv, kv.k, ahead[0], h, wave, lane), v0 = fetch_codes(kv, kv.v, ahead[0], h, wave, lane),
+                  k1 = fetch_codes(kv, kv.k, ahead[1], h, wave, lane);
+      ck[0] = fetch_codes(kv, kv.k, ahead[2], h, wave, lane);
+      cv[0] = fetch_codes(kv, kv.v, ahead[1], h, wave, lane);
+      ck[1] = fetch_codes(kv, kv.k, ahead[3], h, wave, lane);
+      cv[1] = fetch_codes(kv, kv.v, ahead[2], h, wave, lane);
       put_codes<false>(k0, sh.k[0], wave, lane);
       put_codes<true>(v0, sh.v[0], wave, lane);
       put_codes<false>(k1, sh.k[1], wave, lane);
     } else {
+      const Pages<4>&here = ahead[0], &next = ahead[1];
       fetch_step(kv, kv.k, here, h, ld, ld.k_off, lds_k[0]);
       fetch_step(kv, kv.v, here, h, ld, ld.v_off, lds_v[0]);
       fetch_step(kv, kv.k, next, h, ld, ld.k_off, lds_k[1]);
@@ -803,13 +884,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       float mx;
       rows_scores(sh.k[0], qf, n, hh, s0);
       rows_max<2>(s0, mx);
-      mask_scores(tiles.tile(t_begin) * kBigTile, there(here), s0, mx);
+      mask_scores(tiles.tile(t_begin) * kBigTile, there(ahead[0]), s0, mx);
       rows_settle(mx, at.scale, st);
     }
     __syncthreads();                         // the first step replaces its K tile
     int i = t_begin;
     const auto step = [&](int odd, f32x16 (&s)[2], f32x16 (&nx)[2]) __attribute__((always_inline)) {
-      const int j0 = tiles.tile(i) * kBigTile, ok = there(here);
+      const int j0 = tiles.tile(i) * kBigTile, ok = there(ahead[0]);
       // V of a step that some rows see and some do not: what none sees becomes zero where it lies (a weight of zero would not silence infinity
       // or NaN); if what is left is not finite, the rows that see it have it now, and the step meets the finite part
       if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
@@ -832,31 +913,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           __syncthreads();
         }
       }
-      Codes ck, cv;
       if constexpr (FOUR) {                  // (nobody reads these two tiles in this step)
-        ck = fetch_codes(kv, kv.k, after, h, wave, lane);
-        cv = fetch_codes(kv, kv.v, next, h, wave, lane);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        put_codes<false>(ck[odd], sh.k[odd], wave, ln);
+        put_codes<true>(cv[odd], sh.v[odd ^ 1], wave, ln);
+        ck[odd] = fetch_codes(kv, kv.k, ahead[4], h, wave, lane);
+        cv[odd] = fetch_codes(kv, kv.v, ahead[3], h, wave, lane);
       } else {
-        fetch_step(kv, kv.k, after, h, ld, ld.k_off, lds_k[odd]);
-        fetch_step(kv, kv.v, next, h, ld, ld.v_off, lds_v[odd ^ 1]);
+        fetch_step(kv, kv.k, ahead[2], h, ld, ld.k_off, lds_k[odd]);
+        fetch_step(kv, kv.v, ahead[1], h, ld, ld.v_off, lds_v[odd ^ 1]);
       }
-      here = next;
-      next = after;
-      if (i + 3 < t_end) after = pages_of<4>(kv, b.s, tiles.tile(i + 3));
+#pragma unroll
+      for (int d = 0; d + 1 < kPages; ++d) ahead[d] = ahead[d + 1];
+      if (i + kPages < t_end) ahead[kPages - 1] = pages_of<4>(kv, b.s, tiles.tile(i + kPages));
       if (active) {
         float mx;
-        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, lane, st);      // (past the last step: scores that are not used)
+        int ln = lane;
+        if (FOUR) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
+        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st);      // (past the last step: scores that are not used)
         if (i + 1 < t_end) {
-          mask_scores(tiles.tile(i + 1) * kBigTile, there(here), nx, mx);
+          mask_scores(tiles.tile(i + 1) * kBigTile, there(ahead[0]), nx, mx);
           rows_settle(mx, at.scale, st);
         }
       }
-      if constexpr (FOUR) {
-        put_codes<false>(ck, sh.k[odd], wave, lane);
-        put_codes<true>(cv, sh.v[odd ^ 1], wave, lane);
-      } else {
-        landed();
-      }
+      if constexpr (!FOUR) landed();
       __syncthreads();
       ++i;
     };
@@ -892,27 +973,61 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
-// The chunks' results of a row joined: 16 lanes per row.
+// The parts' results of a row joined: a wavefront per row, four groups of 16 lanes that take every fourth part.  Lane l holds the weights of
+// the parts l, 64 + l, ...
 __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) {
-  const int64_t idx = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int piece = threadIdx.x & 15;
+  const int lane = threadIdx.x & 63, piece = lane & 15;
+  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (idx >= rows) return;
   const int64_t tok = idx / at.n_q_heads;
   if (tok < start_of(kv, 0) || tok >= start_of(kv, kv.n_seqs)) return;
-  const float* ml = at.part_ml + 2 * idx * at.n_chunks;
-  float top = -INFINITY;
-  for (int c = 0; c < at.n_chunks; ++c) top = fmaxf(top, part_max(ml[2 * c], ml[2 * c + 1]));
-  float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < at.n_chunks; ++c) {
-    const float m = part_max(ml[2 * c], ml[2 * c + 1]);
-    if (m == -INFINITY) continue;            // an empty part
-    const float f = __builtin_amdgcn_exp2f(m - top);
-    sum += f * ml[2 * c + 1];
-    const float* po = at.part_o + (idx * at.n_chunks + c) * kHeadDim + 8 * piece;
+  float m[4], l[4], top = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] += f * po[k];
+  for (int k = 0; k < 4; ++k) {
+    const int c = 64 * k + lane;
+    m[k] = -INFINITY;
+    l[k] = 0.f;
+    if (c < at.n_chunks) {
+      const f32x2 x = *reinterpret_cast<const f32x2*>(at.part_ml + 2 * (idx * at.n_chunks + c));
+      m[k] = part_max(x[0], x[1]);
+      l[k] = x[1];
+    }
+    top = fmaxf(top, m[k]);
   }
-  finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const f32x4* parts = reinterpret_cast<const f32x4*>(at.part_o + idx * at.n_chunks * kHeadDim) + 2 * piece;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (64 * k >= at.n_chunks) break;
+    const float f = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - top);
+    sum += f * l[k];
+    const uint64_t full = __ballot(m[k] != -INFINITY);
+    for (uint64_t left = full; left;) {      // the next four parts that have something
+      const int skip = lane >> 4;
+      uint64_t mine = left;
+      for (int d = 0; d < skip; ++d) mine &= mine - 1;
+      for (int d = 0; d < 4; ++d) left &= left - 1;
+      if (!mine) continue;
+      const int c = __ffsll((unsigned long long)mine) - 1;
+      const float w = __shfl(f, c);
+      const f32x4 x = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)], y = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[e] += w * x[e];
+        o[4 + e] += w * y[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    o[e] += __shfl_xor(o[e], 16);
+    o[e] += __shfl_xor(o[e], 32);
+  }
+  if (lane < 16) finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
 }
 
 template <class... A>
@@ -932,16 +1047,15 @@ hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hip
 }
 
 hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st) {
-  const int64_t blocks = p.ids * kv.heads * p.n_chunks;
+  const int64_t blocks = (p.ids * p.n_chunks + 7) / 8 * 8 * kv.heads;
   hipError_t e;
   if (p.block_rows == 128) {
     e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at, (int)(p.ids - 1));
   } else {
-    auto kernel = p.block_rows == 16 ? (four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>)
-                                     : (four ? tdk_kv_attend_rows_kernel<true, 2> : tdk_kv_attend_rows_kernel<false, 2>);
+    auto kernel = p.block_rows == 32 ? tdk_kv_attend_rows_kernel<true, 2> : four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>;
     e = launch(kernel, blocks, 256, st, kv, at);
   }
-  if (e == hipSuccess && p.n_chunks > 1) e = launch(tdk_kv_attend_join_kernel, (p.rows + 15) / 16, 256, st, kv, at, p.rows);
+  if (e == hipSuccess && p.n_chunks > 1) e = launch(tdk_kv_attend_join_kernel, (p.rows + 3) / 4, 256, st, kv, at, p.rows);
   return e;
 }
 

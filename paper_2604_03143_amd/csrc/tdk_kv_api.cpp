@@ -128,8 +128,8 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-// false: bad arguments
-bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, KvAttendPlan& p) {
+// window, n_sink: as in the call; without a window the plan is the one with the most parts.  false: bad arguments
+bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
   const int32_t H = kv->model.num_kv_heads;
   if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_len < 0 || n_q_heads < 1 || n_q_heads % H || n_q_heads > kMaxQHeads) return false;
   p = KvAttendPlan{};
@@ -137,13 +137,20 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   if (b->n_seqs == 0 || b->n_tokens == 0) return true;
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_tokens * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
-  p.block_rows = per_seq <= 16 ? 16 : per_seq <= 64 ? 32 : 128;
+  p.block_rows = per_seq <= 16 ? 16 : per_seq <= 32 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
-  // A sequence is cut where its row blocks alone leave compute units idle: two workgroups of four wavefronts each fit on one.
+  // tokens that a block sees: all, or the window of its rows and the first tokens
+  const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_tokens)) : b->max_len;
+  // A sequence is cut where its row blocks alone do not fill the compute units (two workgroups on each, three of the 4-bit rows kernel), into
+  // pieces of 256 tokens at least: a piece costs a workgroup's start and its partial results' way to memory and back.
+  const int64_t len = std::max<int64_t>(1, seen);
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
-  const int64_t want = ((int64_t)2 * kv->n_cus + blocks - 1) / blocks;
-  const int64_t most = ((int64_t)b->max_len + 255) / 256;      // two 32-token tiles per wavefront at least
-  p.n_chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 256));
+  static const int64_t kT = getenv("KVT") ? atoi(getenv("KVT")) : 0, kM = getenv("KVM") ? atoi(getenv("KVM")) : 256;
+  const int64_t resident = (kT ? kT : kv->format == TDK_KV_MXFP4 && p.block_rows == 16 ? 3 : 2) * kv->n_cus;
+  const int64_t fill = (resident + blocks - 1) / blocks, most = (len + kM - 1) / kM;
+  p.n_chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(fill, most), 256));
+  const int64_t tile = p.block_rows == 128 ? 64 : 32;
+  p.piece_tiles = (int32_t)(((len + tile - 1) / tile + p.n_chunks - 1) / p.n_chunks);
   if (p.n_chunks > 1) {
     p.o_part_ml = up256((size_t)p.rows * p.n_chunks * kHeadDim * sizeof(float));
     p.bytes = p.o_part_ml + up256((size_t)p.rows * p.n_chunks * 2 * sizeof(float));
@@ -196,7 +203,7 @@ tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
 
 size_t tdk_kv_attend_workspace_bytes(const tdk_kv* kv, const tdk_kv_batch* batch, int32_t n_q_heads) {
   KvAttendPlan p;
-  return kv && batch && attend_plan_kv(kv, batch, n_q_heads, p) ? p.bytes : 0;
+  return kv && batch && attend_plan_kv(kv, batch, n_q_heads, 0, 0, p) ? p.bytes : 0;
 }
 
 tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch, const tdk_kv_attend_io* a, void* hip_stream) {
@@ -206,9 +213,10 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     if (st != TDK_OK) return st;
     if (!a) return fail(TDK_ERR_INVALID_ARG, "attend io is NULL");
     KvAttendPlan p;
-    if (!attend_plan_kv(kv, batch, a->n_q_heads, p)) return fail(TDK_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of the KV heads");
     if (!std::isfinite(a->scale)) return fail(TDK_ERR_INVALID_ARG, "scale must be finite");
     if (a->window < 0 || a->n_sink < 0) return fail(TDK_ERR_INVALID_ARG, "window / n_sink is negative");
+    if (!attend_plan_kv(kv, batch, a->n_q_heads, a->window, a->n_sink, p))
+      return fail(TDK_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of the KV heads");
     if (!a->part_out != !a->part_lse) return fail(TDK_ERR_INVALID_ARG, "part_out and part_lse come together");
     if (off(a->part_out, 16) || off(a->part_lse, 4) || off(a->hole, 4) || off(a->lse, 4))
       return fail(TDK_ERR_INVALID_ARG, "attend io: part_out must be 16-byte aligned, part_lse, hole and lse 4-byte");
@@ -221,7 +229,7 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
       if (p.bytes && !a->workspace) return fail(TDK_ERR_INVALID_ARG, "workspace is NULL");
       if (p.bytes && off(a->workspace, 256)) return fail(TDK_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
       if (a->workspace_bytes < p.bytes) return fail(TDK_ERR_INVALID_ARG, "workspace smaller than tdk_kv_attend_workspace_bytes()");
-      if (p.ids * kv->model.num_kv_heads * p.n_chunks > kMaxGrid || p.rows > kMaxGrid)
+      if ((p.ids * p.n_chunks + 8) * kv->model.num_kv_heads > kMaxGrid || p.rows > kMaxGrid)
         return fail(TDK_ERR_UNSUPPORTED, "attention launch larger than a grid");
     }
     st = check_device(kv);
@@ -242,6 +250,8 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     at.window = a->window;
     at.n_sink = a->n_sink;
     at.n_chunks = p.n_chunks;
+    at.piece_tiles = p.piece_tiles;
+    at.n_rest = (int32_t)(p.ids * p.n_chunks);
     at.q_flip = std::signbit(a->scale) ? 1 : 0;
     // (a zero scale, uniform weights, becomes one so small that every scaled score rounds to zero: minus infinity stays what it is)
     at.scale = std::fmax(std::fabs(a->scale), 1e-30f);
