@@ -63,6 +63,7 @@ struct KvAttendDev {
 // How a call of the attention is cut.
 struct KvAttendPlan {
   int32_t block_rows = 16;     // query rows (token, head of the group) per workgroup
+  bool forward = true;         // one block per sequence on average: the blocks in their order (else backward)
   int64_t ids = 0;             // row blocks: an upper bound over all ways the tokens can be spread over the sequences
   int32_t n_chunks = 1;
   int32_t piece_tiles = 1;

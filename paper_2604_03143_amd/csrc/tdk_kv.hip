@@ -376,21 +376,48 @@ __device__ __forceinline__ void put_empty(const KvAttendDev& at, const Block& b,
   *reinterpret_cast<f32x2*>(at.part_ml + 2 * (row * at.n_chunks + chunk)) = f32x2{-INFINITY, 0.f};
 }
 
-// Physical pages of the 16-token groups of a tile, -1 where there is none.  What follows is the same for the whole wavefront: scalar reads.
+// Physical pages of the 16-token groups of a tile, -1 where there is none.
 template <int N>
 struct Pages { int p[N]; };
+
+// The pages of a wavefront's tiles first, first + stride, ... below end: 64 / N tiles' worth in the lanes of one register, those of the tiles behind
+// them in another, by one read each.  (Read tile by tile with scalar loads, every step waits for one: the LDS reads share their
+// counter.)  next() is called for one tile after the other, and get() serves that tile and the 64 / N behind it.
 template <int N>
-__device__ __forceinline__ Pages<N> pages_of(const KvDev& kv, int s, int tile) {
-  Pages<N> o;
-  const int32_t* row = kv.table + (int64_t)s * kv.table_stride;
-#pragma unroll
-  for (int it = 0; it < N; ++it) {
-    const int lp = (16 * N * tile + 16 * it) >> kv.page_shift;
-    const int v = scalar_read(row + min(lp, kv.table_stride - 1));
-    o.p[it] = lp < kv.table_stride && v < kv.pool_pages ? max(v, -1) : -1;
+struct PageList {
+  static constexpr int kTiles = 64 / N;
+  int now, then;           // registers of the current 64 / N tiles and of the next ones
+  int at;                  // place of the current tile in `now`
+  int filled;              // tiles that have been read
+  __device__ __forceinline__ int fill(const KvDev& kv, int s, const Tiles& tiles, int first, int stride, int end, int lane) {
+    const int i = min((int64_t)first + (int64_t)stride * (filled + lane / N), (int64_t)end - 1);
+    filled += kTiles;
+    const int lp = (16 * N * tiles.tile(i) + 16 * (lane % N)) >> kv.page_shift;
+    const int v = kv.table[(int64_t)s * kv.table_stride + min(lp, kv.table_stride - 1)];
+    return lp < kv.table_stride && v < kv.pool_pages ? max(v, -1) : -1;
   }
-  return o;
-}
+  __device__ __forceinline__ void start(const KvDev& kv, int s, const Tiles& tiles, int first, int stride, int end, int lane) {
+    filled = 0;
+    now = fill(kv, s, tiles, first, stride, end, lane);
+    then = now;
+    if (end - first > kTiles * stride) then = fill(kv, s, tiles, first, stride, end, lane);
+    at = 0;
+  }
+  __device__ __forceinline__ void next(const KvDev& kv, int s, const Tiles& tiles, int first, int stride, int end, int lane) {
+    if (++at < kTiles) return;
+    at = 0;
+    now = then;
+    if ((int64_t)end - first > (int64_t)filled * stride) then = fill(kv, s, tiles, first, stride, end, lane);
+  }
+  __device__ __forceinline__ Pages<N> get(int d) const {       // of the d-th tile behind the current one
+    Pages<N> o;
+    const int k = at + d, r = k < kTiles ? now : then, l = (k < kTiles ? k : k - kTiles) * N;
+#pragma unroll
+    for (int it = 0; it < N; ++it) o.p[it] = __builtin_amdgcn_readlane(r, l + it);
+    return o;
+  }
+};
+
 template <int N>
 __device__ __forceinline__ int there(const Pages<N>& pg) {      // bit it: the page of tokens 16 it .. is there
   int ok = 0;
@@ -571,14 +598,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
   }
 
   uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kVsStride;
-  // Two tiles take turns: once the scores of one are there its registers belong to the tile after the next, which travels while this one's
-  // weights and second products run and the other tile is worked on.
-  Raw<FOUR> even, odds;
-  Pages<2> pages{};
+  // kTurns tiles take turns: once the scores of one are there its registers belong to a later tile, which travels while this one's weights
+  // and second products run and the other tiles are worked on.
+  constexpr int kTurns = 2;                  // (three and four: the 4-bit kernel spills and loses 5 and 70 %)
+  Raw<FOUR> raw[kTurns];
   const int first = t_begin + wave;
-  if (first < t_end) load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(first)), h, lane, even);
-  if (first + 4 < t_end) load_tile<FOUR>(kv, pages_of<2>(kv, b.s, tiles.tile(first + 4)), h, lane, odds);
-  if (first + 8 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(first + 8));
+  PageList<2> pages;
+  if (first < t_end) {
+    pages.start(kv, b.s, tiles, first, 4, t_end, lane);
+#pragma unroll
+    for (int d = 0; d < kTurns; ++d)
+      if (first + 4 * d < t_end) load_tile<FOUR>(kv, pages.get(d), h, lane, raw[d]);
+  }
   const auto step = [&](const int i, Raw<FOUR>& cur) __attribute__((always_inline)) {
     const int tile = tiles.tile(i), j0 = tile * kTile, ok = cur.ok;
     const bool masked = ok != 3 || !all_see(at, b, j0, j0 + kTile - 1);
@@ -599,8 +630,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
         for (int rt = 0; rt < NR; ++rt)
           s[rt][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), qf[rt][kk], s[rt][tt], 0, 0, 0);
       }
-    if (i + 8 < t_end) load_tile<FOUR>(kv, pages, h, lane, cur);
-    if (i + 12 < t_end) pages = pages_of<2>(kv, b.s, tiles.tile(i + 12));
+    if (i + 4 * kTurns < t_end) load_tile<FOUR>(kv, pages.get(kTurns), h, lane, cur);
+    pages.next(kv, b.s, tiles, first, 4, t_end, lane);
     bf16x8 pb[NR];
     uint32_t live[NR];
 #pragma unroll
@@ -679,9 +710,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
         st[rt].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[rt], st[rt].o[e], 0, 0, 0);
     }
   };
-  for (int i = first; i < t_end; i += 8) {
-    step(i, even);
-    if (i + 4 < t_end) step(i + 4, odds);
+  for (int i = first; i < t_end; i += 4 * kTurns) {
+#pragma unroll
+    for (int d = 0; d < kTurns; ++d)
+      if (i + 4 * d < t_end) step(i + 4 * d, raw[d]);
   }
 
   // the four wavefronts' rows joined: 16 lanes per row, eight elements each
@@ -797,8 +829,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int rest = rest_of<false>(kv.heads, h), chunk = rest % at.n_chunks;
   if (rest >= at.n_rest) return;
   Block b;
-  // (a causal prompt's last rows see most: they start first)
-  if (!find_block(kv, at, last_id - rest / at.n_chunks, kBlockRows, lane, b)) return;
+  // (several blocks per sequence: a causal prompt's last rows see most and start first; one: the numbers without a block come last, ahead of
+  // the others they leave some compute units with one workgroup and others with three; 64 sequences of 4000 tokens, 20 rows: 274 -> 202 us)
+  const int place = rest / at.n_chunks;
+  if (!find_block(kv, at, last_id < 0 ? place : last_id - place, kBlockRows, lane, b)) return;
   h = (h + b.s + chunk) % kv.heads;
   const Tiles tiles = tiles_of(kv, at, b, kBigTile);
   int t_begin, t_end;
@@ -854,26 +888,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     rows_max<2>(s, mx);
   };
 
-  constexpr int kPages = FOUR ? 5 : 3;
   if (t_begin < t_end) {
     f32x16 s0[2], s1[2];
-    // Pages of this step and the next ones.  (Behind the last step the last one's are read again: what that gives is not used.)
-    Pages<4> ahead[5];
-#pragma unroll
-    for (int d = 0; d < 5; ++d) ahead[d] = d < kPages ? pages_of<4>(kv, b.s, tiles.tile(min(t_begin + d, t_end - 1))) : Pages<4>{};
+    // (Behind the last step the last one's pages are read again: what that gives is not used.)
+    PageList<4> pages;
+    pages.start(kv, b.s, tiles, t_begin, 1, t_end, lane);
+    int ok = there(pages.get(0));
     Codes ck[2], cv[2];                      // 4 bits: K of the step behind the next and V of the next one, and both of the step after
     if constexpr (FOUR) {
-      const Codes k0 = fetch_codes(kv, kv.k, ahead[0], h, wave, lane), v0 = fetch_codes(kv, kv.v, ahead[0], h, wave, lane),
-                  k1 = fetch_codes(kv, kv.k, ahead[1], h, wave, lane);
-      ck[0] = fetch_codes(kv, kv.k, ahead[2], h, wave, lane);
-      cv[0] = fetch_codes(kv, kv.v, ahead[1], h, wave, lane);
-      ck[1] = fetch_codes(kv, kv.k, ahead[3], h, wave, lane);
-      cv[1] = fetch_codes(kv, kv.v, ahead[2], h, wave, lane);
+      const Codes k0 = fetch_codes(kv, kv.k, pages.get(0), h, wave, lane), v0 = fetch_codes(kv, kv.v, pages.get(0), h, wave, lane),
+                  k1 = fetch_codes(kv, kv.k, pages.get(1), h, wave, lane);
+      ck[0] = fetch_codes(kv, kv.k, pages.get(2), h, wave, lane);
+      cv[0] = fetch_codes(kv, kv.v, pages.get(1), h, wave, lane);
+      ck[1] = fetch_codes(kv, kv.k, pages.get(3), h, wave, lane);
+      cv[1] = fetch_codes(kv, kv.v, pages.get(2), h, wave, lane);
       put_codes<false>(k0, sh.k[0], wave, lane);
       put_codes<true>(v0, sh.v[0], wave, lane);
       put_codes<false>(k1, sh.k[1], wave, lane);
     } else {
-      const Pages<4>&here = ahead[0], &next = ahead[1];
+      const Pages<4> here = pages.get(0), next = pages.get(1);
       fetch_step(kv, kv.k, here, h, ld, ld.k_off, lds_k[0]);
       fetch_step(kv, kv.v, here, h, ld, ld.v_off, lds_v[0]);
       fetch_step(kv, kv.k, next, h, ld, ld.k_off, lds_k[1]);
@@ -884,13 +917,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       float mx;
       rows_scores(sh.k[0], qf, n, hh, s0);
       rows_max<2>(s0, mx);
-      mask_scores(tiles.tile(t_begin) * kBigTile, there(ahead[0]), s0, mx);
+      mask_scores(tiles.tile(t_begin) * kBigTile, ok, s0, mx);
       rows_settle(mx, at.scale, st);
     }
     __syncthreads();                         // the first step replaces its K tile
     int i = t_begin;
     const auto step = [&](int odd, f32x16 (&s)[2], f32x16 (&nx)[2]) __attribute__((always_inline)) {
-      const int j0 = tiles.tile(i) * kBigTile, ok = there(ahead[0]);
+      const int j0 = tiles.tile(i) * kBigTile;
       // V of a step that some rows see and some do not: what none sees becomes zero where it lies (a weight of zero would not silence infinity
       // or NaN); if what is left is not finite, the rows that see it have it now, and the step meets the finite part
       if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
@@ -918,22 +951,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         asm volatile("" : "+v"(ln));
         put_codes<false>(ck[odd], sh.k[odd], wave, ln);
         put_codes<true>(cv[odd], sh.v[odd ^ 1], wave, ln);
-        ck[odd] = fetch_codes(kv, kv.k, ahead[4], h, wave, lane);
-        cv[odd] = fetch_codes(kv, kv.v, ahead[3], h, wave, lane);
+        ck[odd] = fetch_codes(kv, kv.k, pages.get(4), h, wave, lane);
+        cv[odd] = fetch_codes(kv, kv.v, pages.get(3), h, wave, lane);
       } else {
-        fetch_step(kv, kv.k, ahead[2], h, ld, ld.k_off, lds_k[odd]);
-        fetch_step(kv, kv.v, ahead[1], h, ld, ld.v_off, lds_v[odd ^ 1]);
+        fetch_step(kv, kv.k, pages.get(2), h, ld, ld.k_off, lds_k[odd]);
+        fetch_step(kv, kv.v, pages.get(1), h, ld, ld.v_off, lds_v[odd ^ 1]);
       }
-#pragma unroll
-      for (int d = 0; d + 1 < kPages; ++d) ahead[d] = ahead[d + 1];
-      if (i + kPages < t_end) ahead[kPages - 1] = pages_of<4>(kv, b.s, tiles.tile(i + kPages));
+      pages.next(kv, b.s, tiles, t_begin, 1, t_end, lane);
+      ok = there(pages.get(0));
       if (active) {
         float mx;
         int ln = lane;
         if (FOUR) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
         rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st);      // (past the last step: scores that are not used)
         if (i + 1 < t_end) {
-          mask_scores(tiles.tile(i + 1) * kBigTile, there(ahead[0]), nx, mx);
+          mask_scores(tiles.tile(i + 1) * kBigTile, ok, nx, mx);
           rows_settle(mx, at.scale, st);
         }
       }
@@ -1050,7 +1082,7 @@ hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAtte
   const int64_t blocks = (p.ids * p.n_chunks + 7) / 8 * 8 * kv.heads;
   hipError_t e;
   if (p.block_rows == 128) {
-    e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at, (int)(p.ids - 1));
+    e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at, p.forward ? -1 : (int)(p.ids - 1));
   } else {
     auto kernel = p.block_rows == 32 ? tdk_kv_attend_rows_kernel<true, 2> : four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>;
     e = launch(kernel, blocks, 256, st, kv, at);

@@ -128,6 +128,31 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Into how many parts each sequence is cut, at most (256 tokens a part at least).
+//   Blocks of one sequence each (decoding, drafted tokens): a launch goes round by round, `resident` workgroups at a time (two per compute unit,
+//   three of the 4-bit rows kernel), each as long as a part and what a part costs besides: its workgroup's start and its rows' partial results on
+//   their way to memory and back, here in tokens.  The last round ends late on some compute units, a tenth of a round; so
+//   many parts pay where there are few rounds (64 sequences of 16 000 tokens, one round 725 us, four 680; 66 of 4000 with 20 rows,
+//   one part 275, six 213), and not where there are many (250 of 4000: one part 512, two 529).
+//   Several blocks per sequence (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
+//   many (four prompts of 2048 tokens: one part 508 us, two 629).
+int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
+  const bool four = kv->format == TDK_KV_MXFP4;
+  const int64_t resident = (four && block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus;
+  const int64_t most = std::min<int64_t>((len + 255) / 256, 256);
+  if (per_seq > block_rows || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
+  const double extra = four ? 360 + 8.0 * per_seq : 120 + 2.0 * per_seq;
+  int64_t best = 1;
+  double least = INFINITY;
+  for (int64_t c = 1; c <= most; ++c) {
+    const int64_t rounds = (blocks * c + resident - 1) / resident;
+    const double cost = rounds * ((double)len / c + (c > 1 ? extra : 0.0)) * (1.0 + 0.1 / rounds);
+    if (cost < least) { least = cost; best = c; }
+    if (rounds > 16) break;
+  }
+  return best;
+}
+
 // window, n_sink: as in the call; without a window the plan is the one with the most parts.  false: bad arguments
 bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
   const int32_t H = kv->model.num_kv_heads;
@@ -138,17 +163,13 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_tokens * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
   p.block_rows = per_seq <= 16 ? 16 : per_seq <= 32 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
+  p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // tokens that a block sees: all, or the window of its rows and the first tokens
   const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_tokens)) : b->max_len;
-  // A sequence is cut where its row blocks alone do not fill the compute units (two workgroups on each, three of the 4-bit rows kernel), into
-  // pieces of 256 tokens at least: a piece costs a workgroup's start and its partial results' way to memory and back.
   const int64_t len = std::max<int64_t>(1, seen);
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
-  static const int64_t kT = getenv("KVT") ? atoi(getenv("KVT")) : 0, kM = getenv("KVM") ? atoi(getenv("KVM")) : 256;
-  const int64_t resident = (kT ? kT : kv->format == TDK_KV_MXFP4 && p.block_rows == 16 ? 3 : 2) * kv->n_cus;
-  const int64_t fill = (resident + blocks - 1) / blocks, most = (len + kM - 1) / kM;
-  p.n_chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(fill, most), 256));
+  p.n_chunks = (int32_t)attend_parts(kv, blocks, len, per_seq, p.block_rows);
   const int64_t tile = p.block_rows == 128 ? 64 : 32;
   p.piece_tiles = (int32_t)(((len + tile - 1) / tile + p.n_chunks - 1) / p.n_chunks);
   if (p.n_chunks > 1) {
