@@ -16,9 +16,18 @@ namespace {
 constexpr int kRow = 2 * kHeadDim;         // bytes of a bf16 head row
 constexpr int kRow4 = kHeadDim / 2;        // bytes of its 4-bit values
 
-// A load that passes the caches by, for what is read once.
+// Accesses that pass the caches by, for what is met once.
 template <class T>
 __device__ __forceinline__ T load_once(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(p)); }
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const char* p) {
+  return ONCE ? load_once<u32x4>(p) : *reinterpret_cast<const u32x4*>(p);
+}
+template <bool ONCE>
+__device__ __forceinline__ void store16(char* p, u32x4 v) {
+  if (ONCE) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = v;
+}
 
 // For i in [0, n), at(i) not decreasing: how many are <= x.  The lanes of a wavefront probe 64 places a round (one round up to
 // 64 entries, two up to 4096).  A round leaves less than a 64th of the range, whatever the values are.
@@ -115,11 +124,26 @@ __device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
 // 64 + 8 c .. + 7 of head 8 step + hl of the list K heads, Q heads, V heads: both halves of every pair of either style.
 // Every lane evaluates one of the 64 angles in double and passes cosine and sine (rounded to fp32 once) on through LDS.
 // ---------------------------------------------------------------------------------------------
-template <bool FOUR>
+template <bool FOUR, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const KvRowsDev rows) {
   __shared__ float2 turn[kHalf];
   const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
   const int row = blockIdx.x / rows.waves, part = blockIdx.x - row * rows.waves;
+  const int H = kv.heads, HQ = rows.n_q_heads, n = 2 * H + HQ;
+  // A step's source rows.  They do not depend on where the token goes: the first step's are asked for before that is looked up, every later
+  // one's while the step before it is worked on.
+  const auto load = [&](int step, u32x4& a, u32x4& b) __attribute__((always_inline)) {
+    const int e = 8 * step + hl;
+    a = b = u32x4{0, 0, 0, 0};
+    if (e >= n) return;
+    const bool is_k = e < H, is_q = !is_k && e < H + HQ;
+    const int h = is_k ? e : is_q ? e - H : e - H - HQ;
+    const char* src = is_k ? rows.k + row * rows.k_stride : is_q ? rows.q + row * rows.q_stride : rows.v + row * rows.v_stride;
+    a = load16<ONCE>(src + h * kRow + 16 * c);
+    b = load16<ONCE>(src + h * kRow + 16 * c + 128);
+  };
+  u32x4 na, nb;
+  load(part, na, nb);
   const Slot o = slot_of(kv, row, lane);
   if (o.pos < 0) return;                             // (the queries of a token with no page are rotated all the same)
   double sn, cs;
@@ -129,16 +153,18 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
   float2 t[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) t[i] = turn[kv.interleaved ? 4 * c + (i & 3) + 32 * (i >> 2) : 8 * c + i];
-  const int H = kv.heads, HQ = rows.n_q_heads, n = 2 * H + HQ;
   for (int step = part; 8 * step < n; step += rows.waves) {
     const int e = 8 * step + hl;
     const bool is_k = e < H, is_q = !is_k && e < H + HQ, on = e < n;
     const int h = is_k ? e : is_q ? e - H : e - H - HQ;
-    u32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-    if (on) {
-      const char* src = is_k ? rows.k + row * rows.k_stride : is_q ? rows.q + row * rows.q_stride : rows.v + row * rows.v_stride;
-      a = *reinterpret_cast<const u32x4*>(src + h * kRow + 16 * c);
-      b = *reinterpret_cast<const u32x4*>(src + h * kRow + 16 * c + 128);
+    u32x4 a = na, b = nb;
+    load(step + rows.waves, na, nb);
+    if (!FOUR && !is_k && !is_q) {                   // values move as they are
+      if (!on || o.page < 0) continue;
+      char* dst = kv.v + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow + 16 * c;
+      store16<ONCE>(dst, a);
+      store16<ONCE>(dst + 128, b);
+      continue;
     }
     float x[8], y[8];
 #pragma unroll
@@ -166,21 +192,15 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
       }
     }
     if (!FOUR || is_q) {
-      if (!on || (!is_q && o.page < 0)) continue;
-      char* dst = is_q ? rows.q_out + row * rows.q_out_stride + h * kRow
-                       : (is_k ? kv.k : kv.v) + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow;
+      if (!on || (is_k && o.page < 0)) continue;
+      char* dst = is_q ? rows.q_out + row * rows.q_out_stride + h * kRow : kv.k + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         a[i] = pack2(x[2 * i], x[2 * i + 1]);
         b[i] = pack2(y[2 * i], y[2 * i + 1]);
       }
-      if (!is_k && !is_q) {                          // values move as they are, NaN payloads included
-        const char* src = rows.v + row * rows.v_stride + h * kRow + 16 * c;
-        a = *reinterpret_cast<const u32x4*>(src);
-        b = *reinterpret_cast<const u32x4*>(src + 128);
-      }
-      *reinterpret_cast<u32x4*>(dst + 16 * c) = a;
-      *reinterpret_cast<u32x4*>(dst + 16 * c + 128) = b;
+      store16<ONCE>(dst + 16 * c, a);
+      store16<ONCE>(dst + 16 * c + 128, b);
     } else {
       // (lanes of one block always take the same way here: they hold the same head)
       const uint32_t ex = block_exponent(top_bits(x)), ey = block_exponent(top_bits(y));
@@ -196,7 +216,7 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
 }
 
 // Read: the same lanes, from the cache to rows.
-template <bool FOUR>
+template <bool FOUR, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const KvRowsDev rows) {
   const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
   const int row = blockIdx.x / rows.waves, part = blockIdx.x - row * rows.waves;
@@ -219,13 +239,13 @@ __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const K
         b = from4(*reinterpret_cast<const uint32_t*>(src + 32 + 4 * c), ex >> (8 * (c >> 2) + 16) & 255u);
       } else {
         const char* src = plane + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow + 16 * c;
-        a = *reinterpret_cast<const u32x4*>(src);
-        b = *reinterpret_cast<const u32x4*>(src + 128);
+        a = load16<ONCE>(src);
+        b = load16<ONCE>(src + 128);
       }
     }
     char* dst = (is_k ? rows.k + row * rows.k_stride : rows.v + row * rows.v_stride) + h * kRow + 16 * c;
-    *reinterpret_cast<u32x4*>(dst) = a;
-    *reinterpret_cast<u32x4*>(dst + 128) = b;
+    store16<ONCE>(dst, a);
+    store16<ONCE>(dst + 128, b);
   }
 }
 
@@ -257,17 +277,19 @@ __device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& a
     if (b.s < 0) return false;
     r0 = (e - (int64_t)start_of(kv, b.s) * at.group / block_rows + 1) * block_rows;
   }
-  b.q0 = min(max(scalar_read(kv.q_start + b.s), 0), kv.n_tokens);
-  const int n = min(max(scalar_read(kv.q_start + b.s + 1), 0), kv.n_tokens) - b.q0;
-  if (n <= 0) return false;
+  // (all that depends on the sequence alone is asked for at once)
+  const int q0 = scalar_read(kv.q_start + b.s), q1 = scalar_read(kv.q_start + b.s + 1), len = scalar_read(kv.seq_len + b.s);
+  const int hole_b = at.hole ? scalar_read(at.hole + 2 * b.s) : 0, hole_e = at.hole ? scalar_read(at.hole + 2 * b.s + 1) : 0;
+  b.q0 = min(max(q0, 0), kv.n_tokens);
+  const int n = min(max(q1, 0), kv.n_tokens) - b.q0;
   b.n_rows = n * at.group;                   // (at most n_tokens * n_q_heads, which the host has checked)
-  if (r0 >= b.n_rows) return false;
+  if (n <= 0 || r0 >= b.n_rows) return false;
   b.r0 = (int)r0;
-  b.pos0 = max(scalar_read(kv.seq_len + b.s), 0) - n;      // (tokens of a call and of a table are at most 2^30: differences of positions fit)
+  b.pos0 = max(len, 0) - n;                  // (tokens of a call and of a table are at most 2^30: differences of positions fit)
   b.p_lo = b.pos0 + b.r0 / at.group;
   b.p_hi = b.pos0 + (min(b.r0 + block_rows, b.n_rows) - 1) / at.group;
-  b.hole_b = at.hole ? scalar_read(at.hole + 2 * b.s) : 0;
-  b.hole_e = at.hole ? max(scalar_read(at.hole + 2 * b.s + 1), b.hole_b) : 0;
+  b.hole_b = hole_b;
+  b.hole_e = max(hole_e, hole_b);
   return true;
 }
 
@@ -1070,12 +1092,18 @@ hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t
 
 }  // namespace
 
+// (a wavefront per token: a call so large that the caches would hold nothing of it for whoever comes next; passed by, 12 500 tokens
+// 79 -> 74 us, 20 000 in 4 bits and back 132 -> 118)
 hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
-  return launch(four ? tdk_kv_append_kernel<true> : tdk_kv_append_kernel<false>, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
+  auto kernel = rows.waves == 1 ? (four ? tdk_kv_append_kernel<true, true> : tdk_kv_append_kernel<false, true>)
+                                : (four ? tdk_kv_append_kernel<true, false> : tdk_kv_append_kernel<false, false>);
+  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
 }
 
 hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
-  return launch(four ? tdk_kv_read_kernel<true> : tdk_kv_read_kernel<false>, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
+  auto kernel = rows.waves == 1 ? (four ? tdk_kv_read_kernel<true, true> : tdk_kv_read_kernel<false, true>)
+                                : (four ? tdk_kv_read_kernel<true, false> : tdk_kv_read_kernel<false, false>);
+  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
 }
 
 hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st) {
