@@ -119,6 +119,8 @@ __device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3))};
 }
 
+}  // namespace
+
 // ---------------------------------------------------------------------------------------------
 // Append: a token's K and Q heads rotated, its V heads as they are.  Lane (hl, c) = (lane / 8, lane % 8) holds elements 8 c .. + 7 and
 // 64 + 8 c .. + 7 of head 8 step + hl of the list K heads, Q heads, V heads: both halves of every pair of either style.
@@ -215,6 +217,7 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
   }
 }
 
+
 // Read: the same lanes, from the cache to rows.
 template <bool FOUR, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const KvRowsDev rows) {
@@ -248,6 +251,8 @@ __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const K
     store16<ONCE>(dst + 128, b);
   }
 }
+
+namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Attention.  The query rows of a sequence and KV head are its (token, head of the group) pairs, tokens first; a workgroup takes a
@@ -568,6 +573,8 @@ __device__ __forceinline__ int rest_of(int heads, int& h) {
   return (k & ~7) | ((k + (k >> 3)) & 7);
 }
 
+}  // namespace
+
 // Few query rows (decoding, drafted tokens): a wavefront holds NR tiles of 16 rows and takes every fourth 32-token tile of the workgroup's
 // part; the four join at the end.  K goes from memory into the operands of the products as it lies there (S^T = K Q^T: lane (n, g) then
 // holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.
@@ -772,6 +779,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
   }
 }
 
+namespace {
+
 // ---------------------------------------------------------------------------------------------
 // Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS (tdk_tiles.h): the score products of the next
 // step stand beside the weights and second products of this one, and the pages of the steps behind those travel to LDS meanwhile; 4-bit
@@ -841,6 +850,8 @@ __device__ __forceinline__ void add_odd(const unsigned char* Vs, uint32_t live, 
     }
   }
 }
+
+}  // namespace
 
 template <bool FOUR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_tile_kernel(const KvDev kv, const KvAttendDev at,
@@ -1027,6 +1038,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
+
 // The parts' results of a row joined: a wavefront per row, four groups of 16 lanes that take every fourth part.  Lane l holds the weights of
 // the parts l, 64 + l, ...
 __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) {
@@ -1083,6 +1095,8 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv,
   }
   if (lane < 16) finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
 }
+
+namespace {
 
 template <class... A>
 hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t st, std::common_type_t<A>... args) {
