@@ -792,7 +792,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct StepShared {
   unsigned char k[2][kStepTile];
   unsigned char v[2][kStepTile];
-  int odd[4];
+  int odd[2][4];                             // per V tile and wavefront: it holds infinity or NaN that only some rows may meet
 };
 
 // One plane's 64 tokens of a step: bf16 straight into the LDS tile.  Page groups: 16 tokens, one of the four parts of the tile each.  A page that
@@ -901,24 +901,70 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const StepLoader ld(kv.heads);
   const uint32_t lds_k[2] = {lds_byte(sh.k[0]), lds_byte(sh.k[1])}, lds_v[2] = {lds_byte(sh.v[0]), lds_byte(sh.v[1])};
 
-  // The tokens of a step that the lane's row sees.  kinds: which tests the step needs (first bit: the end, second: window, third: hole or pages)
+  // The tokens of a step that the lane's row sees: bit i is token 32 (i / 16) + 8 ((i % 16) / 4) + 4 hh + i % 4.
+  const auto token = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };
   const auto live_of = [&](int j0, int ok) __attribute__((always_inline)) {
     const int a = pos - j0 - 4 * hh, sink = at.n_sink - j0 - 4 * hh, hb = b.hole_b - j0 - 4 * hh, he = b.hole_e - j0 - 4 * hh;
     uint32_t live = 0;
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
-      const int t = 32 * (k >> 4) + 8 * ((k & 15) >> 2) + (k & 3);
+      const int t = token(k);
       if (t <= a && (at.window == 0 || a - t < at.window || t < sink) && !(t >= hb && t < he) && (ok >> (t >> 4) & 1)) live |= 1u << k;
     }
     return live;
   };
+  // Scores of what the row does not see.  Each kind of border in a pass of its own, for the few steps that meet it: all of them together cost
+  // more than half a step (8192 tokens, a window of 1024: 281 -> 259 us, together with V checked where it is brought).
   const auto mask_scores = [&](int j0, int ok, f32x16 (&s)[2], float& mx) __attribute__((always_inline)) {
-    if (ok == 15 && all_see(at, w, j0, j0 + kBigTile - 1)) return;
-    const uint32_t live = live_of(j0, ok);
+    const int j1 = j0 + kBigTile - 1;
+    if (ok == 15 && all_see(at, w, j0, j1)) return;
+    const int a = pos - j0 - 4 * hh;
+    if (j1 > w.p_lo) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
-      if (!(live >> k & 1)) s[k >> 4][k & 15] = -INFINITY;
+      for (int k = 0; k < 32; ++k) s[k >> 4][k & 15] = token(k) <= a ? s[k >> 4][k & 15] : -INFINITY;
+    }
+    if (at.window && w.p_hi - j0 >= at.window && j1 >= at.n_sink) {
+      const int low = a - at.window, sink = at.n_sink - j0 - 4 * hh;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) s[k >> 4][k & 15] = token(k) > low || token(k) < sink ? s[k >> 4][k & 15] : -INFINITY;
+    }
+    if (ok != 15 || (j1 >= b.hole_b && j0 < b.hole_e)) {
+      const int hb = b.hole_b - j0 - 4 * hh, he = b.hole_e - j0 - 4 * hh;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const int t = token(k);
+        s[k >> 4][k & 15] = !(t >= hb && t < he) && (ok >> (t >> 4) & 1) ? s[k >> 4][k & 15] : -INFINITY;
+      }
+    }
     rows_max<2>(s, mx);
+  };
+  // V of a step that some rows see and some do not, before the barrier that hands it over, by the threads that have brought it: what none
+  // sees becomes zero (a weight of zero would not silence infinity or NaN), and the tile's flag says whether what is left is finite.
+  const auto check_v = [&](int i, int ok, int buf) __attribute__((always_inline)) {
+    const int j0 = tiles.tile(i) * kBigTile;
+    int any = 0;
+    if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
+      u32x4* own = reinterpret_cast<u32x4*>(sh.v[buf] + 16 * threadIdx.x);
+      bool mine = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const u32x4 x = own[256 * e];
+        if (!((ok >> e & 1) && one_sees(at, b, j0 + 16 * e + (int)(threadIdx.x >> 4)))) own[256 * e] = u32x4{0, 0, 0, 0};
+        else mine |= odd16(x[0]) || odd16(x[1]) || odd16(x[2]) || odd16(x[3]);
+      }
+      any = __any(mine);
+    }
+    if (lane == 0) sh.odd[buf][wave] = any;
+  };
+  // the same of 4-bit values, before they are put there
+  const auto check_codes = [&](int i, int ok, int buf, Codes& x) __attribute__((always_inline)) {
+    const int j0 = tiles.tile(i) * kBigTile;
+    int any = 0;
+    if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
+      if (!((ok >> wave & 1) && one_sees(at, b, j0 + 16 * wave + (lane >> 2)))) x = Codes{u32x4{0, 0, 0, 0}, 0};
+      any = __any(x.e == 255);
+    }
+    if (lane == 0) sh.odd[buf][wave] = any;
   };
 
   if (t_begin < t_end) {
@@ -929,13 +975,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     int ok = there(pages.get(0));
     Codes ck[2], cv[2];                      // 4 bits: K of the step behind the next and V of the next one, and both of the step after
     if constexpr (FOUR) {
-      const Codes k0 = fetch_codes(kv, kv.k, pages.get(0), h, wave, lane), v0 = fetch_codes(kv, kv.v, pages.get(0), h, wave, lane),
-                  k1 = fetch_codes(kv, kv.k, pages.get(1), h, wave, lane);
+      const Codes k0 = fetch_codes(kv, kv.k, pages.get(0), h, wave, lane), k1 = fetch_codes(kv, kv.k, pages.get(1), h, wave, lane);
+      Codes v0 = fetch_codes(kv, kv.v, pages.get(0), h, wave, lane);
       ck[0] = fetch_codes(kv, kv.k, pages.get(2), h, wave, lane);
       cv[0] = fetch_codes(kv, kv.v, pages.get(1), h, wave, lane);
       ck[1] = fetch_codes(kv, kv.k, pages.get(3), h, wave, lane);
       cv[1] = fetch_codes(kv, kv.v, pages.get(2), h, wave, lane);
       put_codes<false>(k0, sh.k[0], wave, lane);
+      check_codes(t_begin, ok, 0, v0);
       put_codes<true>(v0, sh.v[0], wave, lane);
       put_codes<false>(k1, sh.k[1], wave, lane);
     } else {
@@ -944,6 +991,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       fetch_step(kv, kv.v, here, h, ld, ld.v_off, lds_v[0]);
       fetch_step(kv, kv.k, next, h, ld, ld.k_off, lds_k[1]);
       landed();
+      check_v(t_begin, ok, 0);
     }
     __syncthreads();
     if (active) {
@@ -956,33 +1004,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     __syncthreads();                         // the first step replaces its K tile
     int i = t_begin;
     const auto step = [&](int odd, f32x16 (&s)[2], f32x16 (&nx)[2]) __attribute__((always_inline)) {
-      const int j0 = tiles.tile(i) * kBigTile;
-      // V of a step that some rows see and some do not: what none sees becomes zero where it lies (a weight of zero would not silence infinity
-      // or NaN); if what is left is not finite, the rows that see it have it now, and the step meets the finite part
-      if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
-        u32x4* own = reinterpret_cast<u32x4*>(sh.v[odd] + 16 * threadIdx.x);
-        bool mine = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const u32x4 x = own[256 * e];
-          if (!((ok >> e & 1) && one_sees(at, b, j0 + 16 * e + (int)(threadIdx.x >> 4)))) own[256 * e] = u32x4{0, 0, 0, 0};
-          else mine |= odd16(x[0]) || odd16(x[1]) || odd16(x[2]) || odd16(x[3]);
-        }
-        const int any = __any(mine);
-        if (lane == 0) sh.odd[wave] = any;
+      if (sh.odd[odd][0] | sh.odd[odd][1] | sh.odd[odd][2] | sh.odd[odd][3]) {
+        // the rows that see what is not finite have it now, and the step meets the rest
+        if (active) add_odd(sh.v[odd], live_of(tiles.tile(i) * kBigTile, ok), lane, st);
         __syncthreads();
-        if (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) {
-          if (active) add_odd(sh.v[odd], live_of(j0, ok), lane, st);
-          __syncthreads();
+        u32x4* own = reinterpret_cast<u32x4*>(sh.v[odd] + 16 * threadIdx.x);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) own[256 * e] = kind_of(own[256 * e], 0);
-          __syncthreads();
-        }
+        for (int e = 0; e < 4; ++e) own[256 * e] = kind_of(own[256 * e], 0);
+        __syncthreads();
       }
+      const int ok_next = there(pages.get(1));
       if constexpr (FOUR) {                  // (nobody reads these two tiles in this step)
         int ln = lane;
         asm volatile("" : "+v"(ln));
         put_codes<false>(ck[odd], sh.k[odd], wave, ln);
+        if (i + 1 < t_end) check_codes(i + 1, ok_next, odd ^ 1, cv[odd]);
         put_codes<true>(cv[odd], sh.v[odd ^ 1], wave, ln);
         ck[odd] = fetch_codes(kv, kv.k, pages.get(4), h, wave, lane);
         cv[odd] = fetch_codes(kv, kv.v, pages.get(3), h, wave, lane);
@@ -991,7 +1027,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         fetch_step(kv, kv.v, pages.get(1), h, ld, ld.v_off, lds_v[odd ^ 1]);
       }
       pages.next(kv, b.s, tiles, t_begin, 1, t_end, lane);
-      ok = there(pages.get(0));
+      ok = ok_next;
       if (active) {
         float mx;
         int ln = lane;
@@ -1002,7 +1038,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           rows_settle(mx, at.scale, st);
         }
       }
-      if constexpr (!FOUR) landed();
+      if constexpr (!FOUR) {
+        landed();
+        if (i + 1 < t_end) check_v(i + 1, ok, odd ^ 1);
+      }
       __syncthreads();
       ++i;
     };
@@ -1069,21 +1108,26 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv,
     if (64 * k >= at.n_chunks) break;
     const float f = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - top);
     sum += f * l[k];
-    const uint64_t full = __ballot(m[k] != -INFINITY);
-    for (uint64_t left = full; left;) {      // the next four parts that have something
-      const int skip = lane >> 4;
-      uint64_t mine = left;
-      for (int d = 0; d < skip; ++d) mine &= mine - 1;
-      for (int d = 0; d < 4; ++d) left &= left - 1;
-      if (!mine) continue;
-      const int c = __ffsll((unsigned long long)mine) - 1;
-      const float w = __shfl(f, c);
-      const f32x4 x = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)], y = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
+    for (int c0 = 0; c0 < 64 && 64 * k + c0 < at.n_chunks; c0 += 16) {
+      // sixteen parts a time, four of them in each lane's hands: their reads are under way together (parts with no weight are not read)
+      f32x4 x[4], y[4];
+      float w[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[e] += w * x[e];
-        o[4 + e] += w * y[e];
+      for (int u = 0; u < 4; ++u) {
+        const int c = c0 + 4 * u + (lane >> 4);
+        w[u] = __shfl(f, c);
+        x[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (w[u] == 0.f) continue;
+        x[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)];
+        y[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
       }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[e] += w[u] * x[u][e];
+          o[4 + e] += w[u] * y[u][e];
+        }
     }
   }
 #pragma unroll
