@@ -293,8 +293,8 @@ __device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& a
   b.pos0 = max(len, 0) - n;                  // (tokens of a call and of a table are at most 2^30: differences of positions fit)
   b.p_lo = b.pos0 + b.r0 / at.group;
   b.p_hi = b.pos0 + (min(b.r0 + block_rows, b.n_rows) - 1) / at.group;
-  b.hole_b = hole_b;
-  b.hole_e = max(hole_e, hole_b);
+  b.hole_b = max(hole_b, 0);
+  b.hole_e = max(hole_e, b.hole_b);
   return true;
 }
 
@@ -924,7 +924,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int k = 0; k < 32; ++k) s[k >> 4][k & 15] = token(k) <= a ? s[k >> 4][k & 15] : -INFINITY;
     }
     if (at.window && w.p_hi - j0 >= at.window && j1 >= at.n_sink) {
-      const int low = a - at.window, sink = at.n_sink - j0 - 4 * hh;
+      const int low = (int)((unsigned)a - (unsigned)at.window), sink = at.n_sink - j0 - 4 * hh;
 #pragma unroll
       for (int k = 0; k < 32; ++k) s[k >> 4][k & 15] = token(k) > low || token(k) < sink ? s[k >> 4][k & 15] : -INFINITY;
     }

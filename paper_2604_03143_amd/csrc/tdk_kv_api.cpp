@@ -275,7 +275,8 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     at.n_rest = (int32_t)(p.ids * p.n_chunks);
     at.q_flip = std::signbit(a->scale) ? 1 : 0;
     // (a zero scale, uniform weights, becomes one so small that every scaled score rounds to zero: minus infinity stays what it is)
-    at.scale = std::fmax(std::fabs(a->scale), 1e-30f);
+    // (and one whose product with log2(e) would overflow the largest that does not: its scores are infinite all the same)
+    at.scale = std::fmin(std::fmax(std::fabs(a->scale), 1e-30f), 2.3e38f);
     at.scale2 = at.scale * 1.4426950408889634f;
     const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->format == TDK_KV_MXFP4, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_attend)");

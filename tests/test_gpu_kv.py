@@ -252,7 +252,8 @@ def test_windows_and_sinks(fmt, window, sink, lengths):
 
 
 @FORMATS
-@pytest.mark.parametrize("hole", [[(0, 0), (5, 5), (0, 32)], [(0, 1000), (32, 64), (1, 250)], [(3, 2), (-5, 17), (17, 2 ** 31 - 1)]])
+@pytest.mark.parametrize("hole", [[(0, 0), (5, 5), (0, 32)], [(0, 1000), (32, 64), (1, 250)], [(3, 2), (-5, 17), (17, 2 ** 31 - 1)],
+                                  [(-2 ** 31, 5), (-2 ** 31, 2 ** 31 - 1), (2 ** 31 - 1, -2 ** 31)]])
 @pytest.mark.parametrize("lengths", [[(0, 1), (90, 1), (250, 1)], [(8, 40), (64, 3), (250, 20)]])
 @pytest.mark.parametrize("window,sink,join", [(0, 0, False), (0, 0, True), (40, 20, True)])
 def test_holes_and_joined_parts(fmt, hole, lengths, window, sink, join):
@@ -261,7 +262,7 @@ def test_holes_and_joined_parts(fmt, hole, lengths, window, sink, join):
 
 
 @FORMATS
-@pytest.mark.parametrize("scale", [0.0, -0.1, 1.0, 3e-39])
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.1, 1.0, 3e-39])
 def test_scales(fmt, scale):
     check_attend(fmt, 2, 4, 16, [(50, 1), (20, 12)], scale=scale)
 

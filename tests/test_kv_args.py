@@ -139,6 +139,23 @@ def test_workspace_depends_on_sizes_alone():
     assert tdk.tdk_kv_attend_workspace_bytes(kv, batch(), 36) == 0
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a machine without a GPU is meant")
+@pytest.mark.parametrize("fmt", [tdk.KV_BF16, tdk.KV_MXFP4])
+def test_the_workspace_serves_every_window(fmt):
+    """A window makes a call shorter, and cuts it otherwise: never into more parts than the workspace that was asked for has room for."""
+    rng = np.random.default_rng(11)
+    for _ in range(3000):
+        heads, seqs = int(rng.choice([1, 2, 3, 8])), int(2 ** rng.uniform(0, 11))
+        group, length = int(rng.choice([1, 4, 5, 8, 16])), int(2 ** rng.uniform(0, 18))
+        tokens = int(rng.choice([seqs, seqs * 3, seqs + 7, seqs * 40]))
+        kv = make(fmt, num_kv_heads=heads)
+        b = batch(n_seqs=seqs, n_tokens=tokens, max_len=length)
+        qd = heads * group * 128
+        need = tdk.tdk_kv_attend_workspace_bytes(kv, b, heads * group)
+        a = io(n_q_heads=heads * group, q_stride=qd, out_stride=qd, window=int(2 ** rng.uniform(0, 18)), n_sink=int(rng.integers(0, 9)), workspace_bytes=need)
+        refused(lambda: tdk.tdk_kv_attend(kv, cache(), b, a), say="device")
+
+
 # ---- the plain forms that the GPU tests compare with, pinned where they can be ----
 
 def test_four_bit_grid_by_hand():
