@@ -526,6 +526,13 @@ __device__ __forceinline__ bool stage_v(const KvAttendDev& at, const Block& b, i
   return masked && b.p_lo != b.p_hi && __any(odd);
 }
 
+// Maximum over the lanes n, n + 16, n + 32, n + 48, by exchanges of registers (through LDS each costs a round trip per tile: with the tests of
+// unmasked tiles gone as well, 64 sequences of 4000 tokens in 4 bits, 20 rows: 70 -> 64 us).
+__device__ __forceinline__ float quad_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
 // Running softmax of 16 query rows: lane (n, g) holds row n; its sum over the lane's own tokens, and elements 16 b + 4 g + i of the
 // un-normalised output.
 struct Rows16 {
@@ -669,24 +676,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
       if (masked) {
         live[rt] = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if ((ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3))) live[rt] |= 1u << k;
+        for (int k = 0; k < 8; ++k) {
+          const bool see = (ok >> (k >> 2) & 1) && sees(at, b, pos[rt], j0 + 16 * (k >> 2) + 4 * g + (k & 3));
+          live[rt] |= (see ? 1u : 0u) << k;
+          s[rt][k >> 2][k & 3] = see ? s[rt][k >> 2][k & 3] : -INFINITY;
+        }
       }
       float p[8], mx = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        p[k] = (live[rt] >> k & 1) ? s[rt][k >> 2][k & 3] * at.scale2 : -INFINITY;
-        mx = fmaxf(mx, p[k]);
-      }
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      for (int k = 0; k < 8; ++k) mx = fmaxf(mx, s[rt][k >> 2][k & 3]);
+      mx = quad_max(mx) * at.scale2;
       // the reference point moves only where a score passes it by 2^8: until then the weights are at most that, in fp32 and bf16 alike
       const float m_new = mx > st[rt].m + 8.f || st[rt].m == -INFINITY ? fmaxf(st[rt].m, mx) : st[rt].m;
       const float ref = m_new == -INFINITY ? 0.f : m_new;
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        p[k] = __builtin_amdgcn_exp2f(p[k] - ref);
+        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][k >> 2][k & 3], at.scale2, -ref));
         sum += p[k];
       }
       if (__any(m_new != st[rt].m)) {

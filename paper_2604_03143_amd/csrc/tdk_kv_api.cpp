@@ -162,7 +162,10 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   if (b->n_seqs == 0 || b->n_tokens == 0) return true;
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_tokens * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
-  p.block_rows = per_seq <= 16 ? 16 : per_seq <= 32 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
+  // (sequences that differ in their new tokens: one token more than the average, so that fewer of them take several blocks; 64 of 4000 tokens,
+  // up to 6 new ones, 5 heads per KV head: 215 -> 147 us, in 4 bits 74 -> 61)
+  const int64_t rows = b->n_tokens > b->n_seqs && b->n_tokens % b->n_seqs ? per_seq + group : per_seq;
+  p.block_rows = rows <= 16 ? 16 : rows <= 32 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // tokens that a block sees: all, or the window of its rows and the first tokens
