@@ -453,6 +453,9 @@ __device__ __forceinline__ int there(const Pages<N>& pg) {      // bit it: the p
   return ok;
 }
 
+constexpr int kRowStride = kHeadDim + 8;   // bf16 elements per staged V row: with 16 bytes behind each, both the writes (16 bytes of sixteen rows, or
+                                           // of a block of four) and the transposing reads (32 bytes of sixteen rows) spread over all banks
+
 // A tile's K and V as they lie in memory.  K: lane (n, g) = (lane % 16, lane / 16) holds token 16 tt + n; bf16: elements 32 kk + 8 g .. + 7 as
 // k[2 kk + tt]; 4 bits: elements 32 g .. + 31 (one block) as k[tt].  V: bf16: lane holds 16 bytes (lane % 16) of token 4 i + lane / 16;
 // 4 bits: block lane % 4 of token 16 i + lane / 4.
@@ -508,7 +511,7 @@ __device__ __forceinline__ bool stage_v(const KvAttendDev& at, const Block& b, i
         r.ve[i] = 0;
       }
       odd |= r.ve[i] == 255;
-      u32x4* dst = reinterpret_cast<u32x4*>(Vs + t * kVsStride + 32 * (lane & 3));
+      u32x4* dst = reinterpret_cast<u32x4*>(Vs + t * kRowStride + 32 * (lane & 3));
 #pragma unroll
       for (int e = 0; e < 4; ++e) dst[e] = from4(r.v[i][e], r.ve[i]);
     }
@@ -520,7 +523,7 @@ __device__ __forceinline__ bool stage_v(const KvAttendDev& at, const Block& b, i
         if (!((r.ok >> (i >> 2) & 1) && one_sees(at, b, tile * kTile + t))) r.v[i] = u32x4{0, 0, 0, 0};
         odd |= odd16(r.v[i][0]) || odd16(r.v[i][1]) || odd16(r.v[i][2]) || odd16(r.v[i][3]);
       }
-      *reinterpret_cast<u32x4*>(Vs + t * kVsStride + 8 * (lane & 15)) = r.v[i];
+      *reinterpret_cast<u32x4*>(Vs + t * kRowStride + 8 * (lane & 15)) = r.v[i];
     }
   }
   return masked && b.p_lo != b.p_hi && __any(odd);
@@ -588,9 +591,9 @@ __device__ __forceinline__ int rest_of(int heads, int& h) {
 template <bool FOUR, int NR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR == 1 ? 3 : 2, FOUR && NR == 1 ? 3 : 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
   constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
-  __shared__ __align__(16) char lds[4 * kTile * kVsStride * 2];
+  __shared__ __align__(16) char lds[4 * kTile * kRowStride * 2];
   __shared__ float ml[4][16][2];
-  static_assert(4 * 16 * kJoin * 4 <= 4 * kTile * kVsStride * 2, "the joining area lies over the V tiles");
+  static_assert(4 * 16 * kJoin * 4 <= 4 * kTile * kRowStride * 2, "the joining area lies over the V tiles");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   int h;
   const int rest = rest_of<FOUR>(kv.heads, h);
@@ -633,7 +636,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
     for (int e = 0; e < 8; ++e) st[rt].o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kVsStride;
+  uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kRowStride;
   // kTurns tiles take turns: once the scores of one are there its registers belong to a later tile, which travels while this one's weights
   // and second products run and the other tiles are worked on.
   constexpr int kTurns = 2;                  // (three and four: the 4-bit kernel spills and loses 5 and 70 %)
@@ -708,10 +711,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
       for (int e = 0; e < 4; ++e) pw[e] = pack2(p[2 * e], p[2 * e + 1]);
       pb[rt] = __builtin_bit_cast(bf16x8, pw);
     }
-    const uint16_t* base = Vs + (4 * g + (n >> 2)) * kVsStride + 4 * (n & 3);
+    const uint16_t* base = Vs + (4 * g + (n >> 2)) * kRowStride + 4 * (n & 3);
     const auto operand = [&](int e) {        // V^T: element 16 e + n of tokens 4 g .. + 3 and 16 + 4 g .. + 3
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * e));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * kVsStride + 16 * e));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + 16 * kRowStride + 16 * e));
       const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
       return u32x4{l2.x, l2.y, h2.x, h2.y};
     };
@@ -732,7 +735,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
       wave_sync();
 #pragma clang loop unroll(disable)
       for (int k = 0; k < 8; ++k) {
-        u32x4* x = reinterpret_cast<u32x4*>(Vs + (4 * k + (lane >> 4)) * kVsStride + 8 * (lane & 15));
+        u32x4* x = reinterpret_cast<u32x4*>(Vs + (4 * k + (lane >> 4)) * kRowStride + 8 * (lane & 15));
         *x = kind_of(*x, 0);
       }
       wave_sync();

@@ -129,18 +129,18 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Into how many parts each sequence is cut, at most (256 tokens a part at least).
-//   Blocks of one sequence each (decoding, drafted tokens): a launch goes round by round, `resident` workgroups at a time (two per compute unit,
+//   Up to 128 rows per sequence (decoding, drafted tokens): a launch goes round by round, `resident` workgroups at a time (two per compute unit,
 //   three of the 4-bit rows kernel), each as long as a part and what a part costs besides: its workgroup's start and its rows' partial results on
 //   their way to memory and back, here in tokens.  The last round ends late on some compute units, a tenth of a round; so
 //   many parts pay where there are few rounds (64 sequences of 16 000 tokens, one round 725 us, four 680; 66 of 4000 with 20 rows,
 //   one part 275, six 213), and not where there are many (250 of 4000: one part 512, two 529).
-//   Several blocks per sequence (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
+//   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
 //   many (four prompts of 2048 tokens: one part 508 us, two 629).
 int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
   const bool four = kv->format == TDK_KV_MXFP4;
   const int64_t resident = (four && block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus;
   const int64_t most = std::min<int64_t>((len + 255) / 256, 256);
-  if (per_seq > block_rows || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
+  if (per_seq > 128 || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
   const double extra = four ? 360 + 8.0 * per_seq : 120 + 2.0 * per_seq;
   int64_t best = 1;
   double least = INFINITY;
@@ -163,9 +163,13 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_tokens * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
   // (sequences that differ in their new tokens: one token more than the average, so that fewer of them take several blocks; 64 of 4000 tokens,
-  // up to 6 new ones, 5 heads per KV head: 215 -> 147 us, in 4 bits 74 -> 61)
+  // up to 6 new ones, 5 heads per KV head: 215 -> 147 us, in 4 bits 74 -> 51)
   const int64_t rows = b->n_tokens > b->n_seqs && b->n_tokens % b->n_seqs ? per_seq + group : per_seq;
-  p.block_rows = rows <= 16 ? 16 : rows <= 32 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
+  // Rows per workgroup.  Up to 16: the rows kernel, which reads K straight into its products.  More: the step kernel, whose 128 rows meet tiles
+  // in LDS; a few of its rows already read at the memory's rate in bf16 (64 sequences of 4000 tokens, 20 rows: 200 us, two passes of 16 rows
+  // over the pages 290).  In 4 bits its tiles come by way of registers, one step ahead of another, and the rows kernel with 32 rows is ahead
+  // up to two blocks (20 rows 61 us against 165; 64 rows 130 against 150; few sequences with 40 to 50 rows are up to 12 % behind).
+  p.block_rows = rows <= 16 ? 16 : rows <= 64 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // tokens that a block sees: all, or the window of its rows and the first tokens

@@ -239,7 +239,8 @@ def test_one_token_per_sequence(fmt, T, H, group):
 @FORMATS
 @pytest.mark.parametrize("T", [16, 32])
 @pytest.mark.parametrize("H,group,lengths", [(2, 5, [(10, 4), (0, 3), (37, 0), (100, 2), (0, 1)]), (8, 1, [(5, 7), (16, 16), (0, 5)]),
-                                             (1, 8, [(0, 40), (33, 50)]), (2, 4, [(0, 131), (70, 66), (5, 1)]), (1, 3, [(0, 300)])])
+                                             (1, 8, [(0, 40), (33, 50)]), (2, 4, [(0, 131), (70, 66), (5, 1)]), (1, 3, [(0, 300)]),
+                                             (2, 8, [(300, 8), (40, 8)]), (3, 16, [(100, 1), (31, 1), (0, 1)]), (2, 16, [(90, 2), (3, 3), (50, 0)]), (8, 5, [(600, 7), (0, 7)])])
 def test_several_tokens_per_sequence(fmt, T, H, group, lengths):
     check_attend(fmt, H, group, T, lengths, pad=2, q_pad=8)
 
