@@ -34,7 +34,7 @@ struct KvRowsDev {
   char*       q_out;
   int64_t     k_stride, v_stride, q_stride, q_out_stride;   // bytes
   int32_t     n_q_heads;       // 0: no queries
-  int32_t     waves;           // wavefronts per token
+  int32_t     waves;           // workgroups per token
   double      inv_freq[kHalf];
 };
 

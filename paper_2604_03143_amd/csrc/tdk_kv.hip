@@ -124,13 +124,21 @@ __device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
 // ---------------------------------------------------------------------------------------------
 // Append: a token's K and Q heads rotated, its V heads as they are.  Lane (hl, c) = (lane / 8, lane % 8) holds elements 8 c .. + 7 and
 // 64 + 8 c .. + 7 of head 8 step + hl of the list K heads, Q heads, V heads: both halves of every pair of either style.
-// Every lane evaluates one of the 64 angles in double and passes cosine and sine (rounded to fp32 once) on through LDS.
+// Every lane evaluates one of the 64 angles in double and passes cosine and sine (rounded to fp32 once) on through LDS: the bits of the rounds'
+// tables for any position, with no table to build or read, and no slower for it (12 500 tokens, a wavefront each: 79.3 us, with no angles at all 79.0).
+// What bounds it: many tokens, the row writes (12 500 tokens with 40 query heads: 391 MB in 68 us, 5.7 TB/s; the counters show no
+// byte more); few, its reads in a row: the starts, the length, the page number (4 tokens 3.7 us, 250 tokens 4.8).
 // ---------------------------------------------------------------------------------------------
 template <bool FOUR, bool ONCE>
-__global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const KvRowsDev rows) {
+__global__ __launch_bounds__(ONCE && !FOUR ? 256 : 64) void tdk_kv_append_kernel(const KvDev kv, const KvRowsDev rows) {
   __shared__ float2 turn[kHalf];
-  const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
-  const int row = blockIdx.x / rows.waves, part = blockIdx.x - row * rows.waves;
+  // Many tokens, bf16: a workgroup of four wavefronts per token, one of which has the angles (the narrower the window of addresses under way, the
+  // faster the writes: 74.5 -> 69.3 us; in 4 bits, with more registers and less to write, 19 000 tokens stored and read back take 116 -> 150,
+  // so there one wavefront has a token).  Few tokens: a workgroup per eight heads.
+  constexpr bool kWide = ONCE && !FOUR;
+  const int lane = threadIdx.x & 63, c = lane & 7, hl = lane >> 3;
+  const int row = kWide ? blockIdx.x : blockIdx.x / rows.waves, part = kWide ? threadIdx.x >> 6 : blockIdx.x - row * rows.waves;
+  const int parts = kWide ? 4 : rows.waves;
   const int H = kv.heads, HQ = rows.n_q_heads, n = 2 * H + HQ;
   // A step's source rows.  They do not depend on where the token goes: the first step's are asked for before that is looked up, every later
   // one's while the step before it is worked on.
@@ -148,19 +156,22 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
   load(part, na, nb);
   const Slot o = slot_of(kv, row, lane);
   if (o.pos < 0) return;                             // (the queries of a token with no page are rotated all the same)
-  double sn, cs;
-  sincos((double)o.pos * rows.inv_freq[lane], &sn, &cs);
-  turn[lane] = make_float2((float)cs, (float)sn);
-  wave_sync();
+  if (!kWide || part == 0) {
+    double sn, cs;
+    sincos((double)o.pos * rows.inv_freq[lane], &sn, &cs);
+    turn[lane] = make_float2((float)cs, (float)sn);
+  }
+  if (kWide) __syncthreads();
+  else wave_sync();
   float2 t[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) t[i] = turn[kv.interleaved ? 4 * c + (i & 3) + 32 * (i >> 2) : 8 * c + i];
-  for (int step = part; 8 * step < n; step += rows.waves) {
+  for (int step = part; 8 * step < n; step += parts) {
     const int e = 8 * step + hl;
     const bool is_k = e < H, is_q = !is_k && e < H + HQ, on = e < n;
     const int h = is_k ? e : is_q ? e - H : e - H - HQ;
     u32x4 a = na, b = nb;
-    load(step + rows.waves, na, nb);
+    load(step + parts, na, nb);
     if (!FOUR && !is_k && !is_q) {                   // values move as they are
       if (!on || o.page < 0) continue;
       char* dst = kv.v + ((((int64_t)o.page << kv.page_shift) + o.at) * H + h) * kRow + 16 * c;
@@ -218,7 +229,7 @@ __global__ __launch_bounds__(64) void tdk_kv_append_kernel(const KvDev kv, const
 }
 
 
-// Read: the same lanes, from the cache to rows.
+// Read: the same lanes, from the cache to rows (19 000 tokens out of 4 bits: 23 us, 4.4 TB/s, nearly all of it writes).
 template <bool FOUR, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const KvRowsDev rows) {
   const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
@@ -587,7 +598,11 @@ __device__ __forceinline__ int rest_of(int heads, int& h) {
 
 // Few query rows (decoding, drafted tokens): a wavefront holds NR tiles of 16 rows and takes every fourth 32-token tile of the workgroup's
 // part; the four join at the end.  K goes from memory into the operands of the products as it lies there (S^T = K Q^T: lane (n, g) then
-// holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.
+// holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.  With at most 16 of 128 rows to
+// share, a page read is used once: nothing is shared between the wavefronts, and none waits for another before the end.
+// What bounds it: the reads.  256 sequences of 4000 tokens, 5 heads per KV head: 6.3 TB/s (one KV head, rows in a run: 6.6), 64 of 16 000 6.2;
+// 250 of 2000 to 4200 tokens 511 us (6.1 TB/s; counters: matrix cores 4 %, vector units 8 % busy).  4 bits: 5.8 TB/s of pages, 6.2 with 32-token pages (vector units
+// 35 %); 32 rows of 64 sequences 61 us (4.7 TB/s), there the vector work of two row tiles.  Few sequences: the start (9 us for 4 of 257 tokens).
 template <bool FOUR, int NR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR == 1 ? 3 : 2, FOUR && NR == 1 ? 3 : 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
   constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
@@ -794,6 +809,9 @@ namespace {
 // Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS (tdk_tiles.h): the score products of the next
 // step stand beside the weights and second products of this one, and the pages of the steps behind those travel to LDS meanwhile; 4-bit
 // pages by way of registers, where they become bf16.
+// What bounds it: the wait between a step's dependent stages, as in the spans' kernel.  Prompts of up to 2048 tokens behind 4000, 5 heads per KV head: 524 us, 845
+// TFLOP/s of what the queries see (counters: matrix cores 35 % busy, vector units 39 %, no bank conflicts; the order of unequal blocks loses a tenth).  Few of the
+// 128 rows in use: the reads (64 sequences of 4000 tokens, 20 rows: 200 us, 5.3 TB/s); in 4 bits the way through registers (150 us, 1.9 TB/s).
 // ---------------------------------------------------------------------------------------------
 constexpr int kBlockRows = 4 * 32;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -1088,7 +1106,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
 
 // The parts' results of a row joined: a wavefront per row, four groups of 16 lanes that take every fourth part.  Lane l holds the weights of
-// the parts l, 64 + l, ...
+// the parts l, 64 + l, ...  Two reads in a row, weights and results (80 rows of 64 parts: 7 us; one part after the other 11, a row per 16 lanes 24).
 __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) {
   const int lane = threadIdx.x & 63, piece = lane & 15;
   const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -1159,12 +1177,12 @@ hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t
 
 }  // namespace
 
-// (a wavefront per token: a call so large that the caches would hold nothing of it for whoever comes next; passed by, 12 500 tokens
-// 79 -> 74 us, 20 000 in 4 bits and back 132 -> 118)
+// (one part per token: a call so large that the caches would hold nothing of it for whoever comes next; passed by, 12 500 tokens
+// 79 -> 74 us, 19 000 in 4 bits and back 132 -> 118)
 hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
   auto kernel = rows.waves == 1 ? (four ? tdk_kv_append_kernel<true, true> : tdk_kv_append_kernel<false, true>)
                                 : (four ? tdk_kv_append_kernel<true, false> : tdk_kv_append_kernel<false, false>);
-  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
+  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, rows.waves == 1 && !four ? 256 : 64, st, kv, rows);
 }
 
 hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {

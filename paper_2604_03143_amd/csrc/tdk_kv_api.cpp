@@ -111,8 +111,8 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
     r.q_out_stride = 2 * rows->q_out_stride;
     r.n_q_heads = rows->n_q_heads;
   }
-  // A wavefront takes eight heads of a token at a time.  Few tokens: one wavefront for each eight heads, so that all of a call's
-  // accesses are under way at once; many: one per token, which has to find out where the token lies and what its angles are once.
+  // A wavefront takes eight heads of a token at a time.  Few tokens: a workgroup for each eight heads, so that all of a call's
+  // accesses are under way at once; many: the token's place and angles are found out once for all its heads.
   const int steps = (2 * kv->model.num_kv_heads + r.n_q_heads + 7) / 8;
   r.waves = (int64_t)batch->n_tokens * steps <= (int64_t)8 * kv->n_cus ? steps : 1;
   if ((int64_t)batch->n_tokens * r.waves > kMaxGrid) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
@@ -133,7 +133,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   three of the 4-bit rows kernel), each as long as a part and what a part costs besides: its workgroup's start and its rows' partial results on
 //   their way to memory and back, here in tokens.  The last round ends late on some compute units, a tenth of a round; so
 //   many parts pay where there are few rounds (64 sequences of 16 000 tokens, one round 725 us, four 680; 66 of 4000 with 20 rows,
-//   one part 275, six 213), and not where there are many (250 of 4000: one part 512, two 529).
+//   one part 275, six 237), and not where there are many (250 of 4000: one part 512, two 529).
 //   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
 //   many (four prompts of 2048 tokens: one part 508 us, two 629).
 int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
