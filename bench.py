@@ -53,7 +53,7 @@ def parse():
 
 
 KERNEL_SOURCES = {"hbm_traffic": ("tdk_kernels.hip", "tdk_internal.h", "tdk_types.h"),
-                  "hbm_traffic_attend": ("tdk_attend.hip", "tdk_internal.h", "tdk_types.h")}
+                  "hbm_traffic_attend": ("tdk_attend.hip", "tdk_tiles.h", "tdk_internal.h", "tdk_types.h")}
 
 
 def csrc_hash(prefix="hbm_traffic"):
