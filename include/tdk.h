@@ -387,11 +387,12 @@ typedef struct {
  * of them are the batch's: its token t (position seq_len[s] - n_s + t) is row q_start[s] + t of the token buffers.
  *   n_tokens   rows of the token buffers; q_start[n_seqs] may be smaller: the rows behind it are left alone
  *   max_len    longest sequence that is expected: how a call is cut into workgroups goes by it and by the
- *              sizes above, results do not (a longer sequence is served too, only more slowly)
+ *              sizes above, and with that the order of its fp32 sums (a longer sequence is served too, only more slowly)
  * Token j lies in physical page block_table[s][j / T].  q_start must not decrease.  Everything on the device is
  * checked there: starts are cut to [0, n_tokens], and a token whose position is negative, whose logical page
  * lies past table_stride or whose page number is not in [0, pool_pages) is not written by append, reads as zero
- * and is seen by no query.  At most 2^30 tokens per call, and per sequence by its table (else UNSUPPORTED). */
+ * and is seen by no query.  At most 2^30 tokens per sequence by its table, and per call what one launch holds: 2^32
+ * threads, 256 for each token that is appended or read (else UNSUPPORTED). */
 typedef struct {
   int32_t        n_seqs;
   int32_t        n_tokens;
@@ -420,7 +421,8 @@ typedef struct {
  * arithmetic above, V as it is; with q, the rotated queries into q_out.  MXFP4: the fp32 values go to the nearest
  * 4-bit value of their block (ties to even); the block's power of two is 2^(floor(log2 m) - 2) of its largest
  * magnitude m, one higher from m = 1.75 * 2^n on (what lies beyond 6 becomes 6); a block with an infinity or NaN
- * becomes NaN.  Tokens must lie in pages that no other token of the batch is written to.  One kernel. */
+ * becomes NaN.  No two tokens of a batch may have the same place in the cache (sequences that
+ * share pages differ in the pages they append to).  One kernel. */
 tdk_status tdk_kv_append(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
                          const tdk_kv_rows* rows, void* hip_stream);
 

@@ -20,7 +20,8 @@ struct tdk_kv {
 
 namespace {
 
-constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;    // workgroups of one launch
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;    // query rows of a call: their numbers are int32
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1; // of one launch
 constexpr int32_t kMaxQHeads = 1 << 16;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;        // of a call, and of a sequence that a table has room for
 
@@ -115,7 +116,7 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
   // accesses are under way at once; many: the token's place and angles are found out once for all its heads.
   const int steps = (2 * kv->model.num_kv_heads + r.n_q_heads + 7) / 8;
   r.waves = (int64_t)batch->n_tokens * steps <= (int64_t)8 * kv->n_cus ? steps : 1;
-  if ((int64_t)batch->n_tokens * r.waves > kMaxGrid) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
+  if ((int64_t)batch->n_tokens * r.waves * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
   std::copy(std::begin(kv->inv_freq), std::end(kv->inv_freq), std::begin(r.inv_freq));
   st = check_device(kv);
   if (st != TDK_OK || nothing) return st;
@@ -257,7 +258,7 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
       if (p.bytes && !a->workspace) return fail(TDK_ERR_INVALID_ARG, "workspace is NULL");
       if (p.bytes && off(a->workspace, 256)) return fail(TDK_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
       if (a->workspace_bytes < p.bytes) return fail(TDK_ERR_INVALID_ARG, "workspace smaller than tdk_kv_attend_workspace_bytes()");
-      if ((p.ids * p.n_chunks + 8) * kv->model.num_kv_heads > kMaxGrid || p.rows > kMaxGrid)
+      if ((p.ids * p.n_chunks + 8) * kv->model.num_kv_heads * 256 > kMaxThreads || p.rows > kMaxRows)
         return fail(TDK_ERR_UNSUPPORTED, "attention launch larger than a grid");
     }
     st = check_device(kv);

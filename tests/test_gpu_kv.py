@@ -246,6 +246,15 @@ def test_several_tokens_per_sequence(fmt, T, H, group, lengths):
 
 
 @FORMATS
+@pytest.mark.parametrize("T,group,lengths,kw", [(16, 33, [(70, 1), (0, 1), (300, 1)], {}), (32, 129, [(40, 1), (90, 2), (5, 0)], dict(window=20, sink=3)),
+                                                (16, 300, [(130, 1), (0, 3)], dict(hole=[(30, 60), (1, 2)], join=True)), (32, 64, [(4000, 1)], {}),
+                                                (16, 160, [(3000, 2)], dict(window=1500, sink=1))])
+def test_more_query_heads_than_a_block_of_rows_holds(fmt, T, group, lengths, kw):
+    """One KV head for all queries: a token's heads fill several blocks, or a block not quite."""
+    check_attend(fmt, 1, group, T, lengths, q_pad=8, **kw)
+
+
+@FORMATS
 @pytest.mark.parametrize("window,sink", [(1, 0), (1, 1), (7, 0), (16, 4), (33, 40), (64, 1), (1000, 5), (2 ** 31 - 1, 0), (5, 2 ** 31 - 1)])
 @pytest.mark.parametrize("lengths", [[(0, 1), (3, 1), (40, 1), (250, 1)], [(0, 70), (90, 40), (7, 3)]])
 def test_windows_and_sinks(fmt, window, sink, lengths):

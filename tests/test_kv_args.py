@@ -114,6 +114,10 @@ def test_too_many_tokens():
         refused(lambda: tdk.tdk_kv_append(kv, cache(), b, rows()), tdk.ERR_UNSUPPORTED)
         refused(lambda: tdk.tdk_kv_attend(kv, cache(), b, io()), tdk.ERR_UNSUPPORTED)
     refused(lambda: tdk.tdk_kv_attend(kv, cache(), batch(n_tokens=1 << 26), io()), tdk.ERR_UNSUPPORTED, "grid")
+    # a launch has fewer than 2^32 threads: 256 per token moved, 256 per block of query rows and KV head (here 2^21 sequences of one block, 8 heads)
+    for f in (tdk.tdk_kv_append, tdk.tdk_kv_read):
+        refused(lambda: f(kv, cache(), batch(n_tokens=1 << 24), rows(q=None, q_out=None)), tdk.ERR_UNSUPPORTED, "launch")
+    refused(lambda: tdk.tdk_kv_attend(kv, cache(), batch(n_seqs=1 << 21, n_tokens=1 << 21), io()), tdk.ERR_UNSUPPORTED, "grid")
 
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="a machine without a GPU is meant")
