@@ -24,6 +24,7 @@ constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;    // query rows of a call:
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1; // of one launch
 constexpr int32_t kMaxQHeads = 1 << 16;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;        // of a call, and of a sequence that a table has room for
+constexpr int32_t kMaxSeqs = 1 << 30;                   // the search for a token's sequence counts in int32, in steps of 64
 
 bool off(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
@@ -37,6 +38,7 @@ tdk_status check_batch(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
   if (cache->pool_pages < 0 || cache->pool_pages >= (int64_t)1 << 31) return fail(TDK_ERR_INVALID_ARG, "cache: pool_pages out of range");
   if (b->n_tokens > kMaxTokens || (int64_t)b->table_stride * kv->model.page_tokens > kMaxTokens)
     return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 tokens");
+  if (b->n_seqs > kMaxSeqs) return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 sequences");
   *nothing = b->n_seqs == 0 || b->n_tokens == 0;
   if (*nothing) return TDK_OK;
   if (!b->q_start || !b->seq_len) return fail(TDK_ERR_INVALID_ARG, "batch: q_start / seq_len is NULL");
