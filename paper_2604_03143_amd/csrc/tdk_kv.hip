@@ -362,9 +362,14 @@ __device__ __forceinline__ bool one_sees(const KvAttendDev& at, const Block& b, 
   return j <= b.p_hi && (at.window == 0 || b.p_lo - j < at.window || j < at.n_sink) && !(j >= b.hole_b && j < b.hole_e);
 }
 
-// log-sum-exp of a row from its maximum in base 2: -infinity for an empty one, NaN for a row with a NaN score
+// The reference point of a row follows its maximum only where a score has passed it by some distance (2^8 in the rows kernel, e^8 = 2^11.5 in
+// the step kernel).  Weights are taken 2^kBelow lower, so that none is above one: with weights of up to e^8, values of 1e35 and more run over in
+// sums that are finite once divided.  Sums and un-normalised outputs carry the factor alike; the logarithm takes it out.
+constexpr float kBelow = 12.f, kRaise = 4096.f;
+
+// log-sum-exp of a row from its reference point in base 2: -infinity for an empty one, NaN for a row with a NaN score
 __device__ __forceinline__ float row_lse2(float m2, float l) {
-  return l > 0.f ? 0.69314718055994531f * m2 + __logf(l) : l != l ? l : -INFINITY;
+  return l > 0.f ? 0.69314718055994531f * m2 + __logf(l * kRaise) : l != l ? l : -INFINITY;
 }
 
 // Eight elements of a finished row (un-normalised sums o, maximum m2, sum l): joined with the caller's partial result and written.
@@ -379,10 +384,10 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
     const float pl = at.other_lse[idx];
     if (pl != -INFINITY) {
       const float top = fmaxf(lse, pl);
-      const float w = __expf(lse - top), pw = __expf(pl - top), both = w + pw;
+      const float w = __expf(lse - top), pw = __expf(pl - top), both = w + pw, wb = w / both, pb = pw / both;
       const float* po = at.other_out + idx * kHeadDim + 8 * piece;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = (w * r[i] + pw * po[i]) / both;
+      for (int i = 0; i < 8; ++i) r[i] = wb * r[i] + pb * po[i];      // (shares first: the two together may be beyond fp32)
       lse = top + __logf(both);
     }
   }
@@ -704,13 +709,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
 #pragma unroll
       for (int k = 0; k < 8; ++k) mx = fmaxf(mx, s[rt][k >> 2][k & 3]);
       mx = quad_max(mx) * at.scale2;
-      // the reference point moves only where a score passes it by 2^8: until then the weights are at most that, in fp32 and bf16 alike
+      // the reference point moves only where a score passes it by 2^8
       const float m_new = mx > st[rt].m + 8.f || st[rt].m == -INFINITY ? fmaxf(st[rt].m, mx) : st[rt].m;
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float ref = m_new == -INFINITY ? 0.f : m_new, m2 = -(ref + kBelow);
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][k >> 2][k & 3], at.scale2, -ref));
+        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][k >> 2][k & 3], at.scale2, m2));
         sum += p[k];
       }
       if (__any(m_new != st[rt].m)) {
@@ -1059,7 +1064,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         float mx;
         int ln = lane;
         if (FOUR) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
-        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st);      // (past the last step: scores that are not used)
+        // (past the last step: scores that are not used)
+        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st, [&] { return -(st.m_run == -INFINITY ? 0.f : st.m_run) * kLog2e - kBelow; });
         if (i + 1 < t_end) {
           mask_scores(tiles.tile(i + 1) * kBigTile, ok, nx, mx);
           rows_settle(mx, at.scale, st);
