@@ -362,7 +362,8 @@ tdk_status tdk_restore_layers(tdk_round* r, int32_t first_layer, int32_t n_layer
  *                  values of its T tokens (64 bytes each, element 2 i in the low half of byte i), then the
  *                  block exponents (4 bytes each).  A value is one sign, two exponent bits and one mantissa bit
  *                  (magnitudes 0 0.5 1 1.5 2 3 4 6); 32 consecutive elements of a row share a power of two
- *                  2^(byte - 127); byte 255 makes all 32 NaN. */
+ *                  2^(byte - 127); byte 255 makes all 32 NaN.  Every call takes values as bf16 has them: exact, and
+ *                  infinite from 2^128 on (bytes 253 and 254). */
 #define TDK_KV_BF16  0
 #define TDK_KV_MXFP4 1
 
@@ -420,14 +421,15 @@ typedef struct {
 /* Writes the batch's tokens into the cache: K (un-rotated in `rows`) rotated for each token's position in the
  * arithmetic above, V as it is; with q, the rotated queries into q_out.  MXFP4: the fp32 values go to the nearest
  * 4-bit value of their block (ties to even); the block's power of two is 2^(floor(log2 m) - 2) of its largest
- * magnitude m, one higher from m = 1.75 * 2^n on (what lies beyond 6 becomes 6); a block with an infinity or NaN
- * becomes NaN.  No two tokens of a batch may have the same place in the cache (sequences that
- * share pages differ in the pages they append to).  One kernel. */
+ * magnitude m, one higher from m = 1.75 * 2^n on (what lies beyond 6 becomes 6), and 2^-126 at least; a block with an
+ * infinity or NaN becomes NaN, and in one with m from 1.75 * 2^127 on what rounds to 2^128 is infinite.  No two
+ * tokens of a batch may have the same place in the cache (sequences that share pages differ in the pages they
+ * append to).  One kernel. */
 tdk_status tdk_kv_append(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
                          const tdk_kv_rows* rows, void* hip_stream);
 
 /* The inverse: the batch's tokens out of the cache into rows->k / rows->v (the same rows that append would take;
- * K stays rotated; 4-bit values are exact in bf16).  rows->q must be NULL.  One kernel. */
+ * K stays rotated; 4-bit values as above).  rows->q must be NULL.  One kernel. */
 tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
                        const tdk_kv_rows* rows, void* hip_stream);
 

@@ -110,7 +110,9 @@ __device__ __forceinline__ uint32_t to4(const float (&x)[8], uint32_t e) {
   return w;
 }
 
-// Eight 4-bit values times their block's power of two, exact in bf16 (a byte of 255 gives NaN).
+// Eight 4-bit values times their block's power of two, exact in bf16 up to its range: a byte of 255 gives NaN, and from kWide4 on (4 * 2^126) some
+// values are infinite.
+constexpr uint32_t kWide4 = 253;
 __device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
   const float unit = __uint_as_float(e << 23);
   return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 0)),
@@ -526,7 +528,7 @@ __device__ __forceinline__ bool stage_v(const KvAttendDev& at, const Block& b, i
         r.v[i] = u32x4{0, 0, 0, 0};
         r.ve[i] = 0;
       }
-      odd |= r.ve[i] == 255;
+      odd |= r.ve[i] >= kWide4;
       u32x4* dst = reinterpret_cast<u32x4*>(Vs + t * kRowStride + 32 * (lane & 3));
 #pragma unroll
       for (int e = 0; e < 4; ++e) dst[e] = from4(r.v[i][e], r.ve[i]);
@@ -994,7 +996,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     int any = 0;
     if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
       if (!((ok >> wave & 1) && one_sees(at, b, j0 + 16 * wave + (lane >> 2)))) x = Codes{u32x4{0, 0, 0, 0}, 0};
-      any = __any(x.e == 255);
+      any = __any(x.e >= kWide4);
     }
     if (lane == 0) sh.odd[buf][wave] = any;
   };
