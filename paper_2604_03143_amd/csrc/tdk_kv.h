@@ -44,7 +44,7 @@ struct KvAttendDev {
   char*          out;
   float*         lse;
   float*         part_o;       // workspace: [n_tokens * n_q_heads][n_chunks][128] un-normalised partial outputs
-  float*         part_ml;      // workspace: [n_tokens * n_q_heads][n_chunks][2] maximum (base 2), sum
+  float*         part_ml;      // workspace: [n_tokens * n_q_heads][n_chunks][2] reference point (a score), sum
   const int32_t* hole;
   const float*   other_out;    // the caller's partial result
   const float*   other_lse;

@@ -269,7 +269,7 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Attention.  The query rows of a sequence and KV head are its (token, head of the group) pairs, tokens first; a workgroup takes a
-// block of them and a part of the tokens they see.  Scores are kept in base 2: s = (q . k) scale log2(e).
+// block of them and a part of the tokens they see.  Scores are kept as the products leave them, unscaled.
 // ---------------------------------------------------------------------------------------------
 // A block of query rows: which sequence it belongs to, and what its rows see.
 struct Block {
@@ -364,29 +364,33 @@ __device__ __forceinline__ bool one_sees(const KvAttendDev& at, const Block& b, 
   return j <= b.p_hi && (at.window == 0 || b.p_lo - j < at.window || j < at.n_sink) && !(j >= b.hole_b && j < b.hole_e);
 }
 
-// The reference point of a row follows its maximum only where a score has passed it by some distance (2^8 in the rows kernel, e^8 = 2^11.5 in
-// the step kernel).  Weights are taken 2^kBelow lower, so that none is above one: with weights of up to e^8, values of 1e35 and more run over in
-// sums that are finite once divided.  Sums and un-normalised outputs carry the factor alike; the logarithm takes it out.
-constexpr float kBelow = 12.f, kRaise = 4096.f;
+// A weight is 2^(scale2 (s - m) - kBelow): s the score q . k as the products leave it, m the row's reference point, which is one of its scores.
+// The difference comes first: it is exact where it matters, and zero at the maximum, whatever the scale.  (Scaled first, s scale2 and m scale2 are
+// rounded apart, and from 2^30 on that is more than all exponents that fp32 has: rows of zeros and of infinities.)
+// The reference point follows the maximum only where a score has passed it by more than 2^kLazy.  Weights are taken 2^kBelow lower, so that none is
+// above one: with weights of up to e^8, values of 1e35 and more run over in sums that are finite once divided.  Sums and un-normalised
+// outputs carry the factor alike; the logarithm takes it out.
+constexpr float kLazy = 11.5f, kBelow = 12.f, kRaise = 4096.f;
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }      // (nothing seen yet: no score above -infinity)
+__device__ __forceinline__ float exponent(float s, float ref, float scale2) { return __builtin_fmaf(s - ref, scale2, -kBelow); }
+__device__ __forceinline__ float moved(float m, float mx, float scale2) { return (mx - m) * scale2 > kLazy ? mx : m; }
+// what sums that go with the reference point m count towards those of a reference point `ref`
+__device__ __forceinline__ float share(float m, float ref, float scale2) { return __builtin_amdgcn_exp2f((m - ref) * scale2); }
 
-// log-sum-exp of a row from its reference point in base 2: -infinity for an empty one, NaN for a row with a NaN score
-__device__ __forceinline__ float row_lse2(float m2, float l) {
-  return l > 0.f ? 0.69314718055994531f * m2 + __logf(l * kRaise) : l != l ? l : -INFINITY;
-}
-
-// Eight elements of a finished row (un-normalised sums o, maximum m2, sum l): joined with the caller's partial result and written.
-__device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int hq, int piece, const float (&o)[8], float m2, float l) {
+// Eight elements of a finished row (un-normalised sums o, reference point m, sum l): joined with the caller's partial result and written.
+__device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int hq, int piece, const float (&o)[8], float m, float l) {
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   float r[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = o[i] * inv;
-  float lse = row_lse2(m2, l);
+  // log-sum-exp: -infinity for an empty row, NaN for one with a NaN score, infinite where fp32 has no such number
+  float lse = l > 0.f ? m * at.scale + __logf(l * kRaise) : l != l ? l : -INFINITY;
   const int64_t idx = tok * at.n_q_heads + hq;
   if (at.other_out) {
     const float pl = at.other_lse[idx];
     if (pl != -INFINITY) {
       const float top = fmaxf(lse, pl);
-      const float w = __expf(lse - top), pw = __expf(pl - top), both = w + pw, wb = w / both, pb = pw / both;
+      const float w = lse == top ? 1.f : __expf(lse - top), pw = pl == top ? 1.f : __expf(pl - top), both = w + pw, wb = w / both, pb = pw / both;
       const float* po = at.other_out + idx * kHeadDim + 8 * piece;
 #pragma unroll
       for (int i = 0; i < 8; ++i) r[i] = wb * r[i] + pb * po[i];      // (shares first: the two together may be beyond fp32)
@@ -401,16 +405,16 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
 }
 
 // The same for a workgroup's part: finished if it is the only one, else kept for the join.
-__device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m2, float l) {
+__device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m, float l) {
   if (at.n_chunks == 1) {
-    finish(at, tok, hq, piece, o, m2, l);
+    finish(at, tok, hq, piece, o, m, l);
     return;
   }
   const int64_t part = (tok * at.n_q_heads + hq) * at.n_chunks + chunk;
   f32x4* dst = reinterpret_cast<f32x4*>(at.part_o + part * kHeadDim + 8 * piece);
   dst[0] = f32x4{o[0], o[1], o[2], o[3]};
   dst[1] = f32x4{o[4], o[5], o[6], o[7]};
-  if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{m2, l};
+  if (piece == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{m, l};
 }
 
 // A part with no tokens: nothing but that is kept of it.
@@ -710,18 +714,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
       float p[8], mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 8; ++k) mx = fmaxf(mx, s[rt][k >> 2][k & 3]);
-      mx = quad_max(mx) * at.scale2;
-      // the reference point moves only where a score passes it by 2^8
-      const float m_new = mx > st[rt].m + 8.f || st[rt].m == -INFINITY ? fmaxf(st[rt].m, mx) : st[rt].m;
-      const float ref = m_new == -INFINITY ? 0.f : m_new, m2 = -(ref + kBelow);
+      const float m_new = moved(st[rt].m, quad_max(mx), at.scale2), ref = reference(m_new);
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][k >> 2][k & 3], at.scale2, m2));
+        p[k] = __builtin_amdgcn_exp2f(exponent(s[rt][k >> 2][k & 3], ref, at.scale2));
         sum += p[k];
       }
       if (__any(m_new != st[rt].m)) {
-        const float alpha = __builtin_amdgcn_exp2f(st[rt].m - ref);
+        const float alpha = share(st[rt].m, ref, at.scale2);
         st[rt].l *= alpha;
 #pragma unroll
         for (int e = 0; e < 8; ++e) st[rt].o[e] *= alpha;
@@ -801,7 +802,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float m = ml[w][row][0];
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      const float f = m == -INFINITY ? 0.f : share(m, top, at.scale2);
       sum += f * ml[w][row][1];
 #pragma unroll
       for (int k = 0; k < 8; ++k) o[k] += f * join[w][row][8 * piece + k];
@@ -821,7 +822,6 @@ namespace {
 // 128 rows in use: the reads (64 sequences of 4000 tokens, 20 rows: 200 us, 5.3 TB/s); in 4 bits the way through registers (150 us, 1.9 TB/s).
 // ---------------------------------------------------------------------------------------------
 constexpr int kBlockRows = 4 * 32;
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct StepShared {
   unsigned char k[2][kStepTile];
@@ -972,6 +972,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     rows_max<2>(s, mx);
   };
+  // The difference of score and reference point costs the step a twentieth (prompts 530 -> 545 us, with a window 259 -> 270), so it is taken where it is
+  // needed: up to 2^12 the product of reference point and scale is rounded by 2^-12 at most, the same for all weights until the point moves.
+  constexpr float kFar = 4096.f;
+  bool far = false;                          // some row of the wavefront is beyond
+  // mx: each lane's maximum of the masked scores to come
+  const auto settle = [&](float mx) __attribute__((always_inline)) {
+    const float m_new = moved(st.m_run, pair_max(mx), at.scale2);
+    if (!__any(m_new != st.m_run)) return;
+    const float alpha = share(st.m_run, reference(m_new), at.scale2);       // 1 for the rows whose reference point stays
+    st.l_run *= alpha;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.oacc[q][i] *= alpha;
+    st.m_run = m_new;
+    far = __any(fabsf(reference(m_new)) * at.scale2 > kFar);
+  };
   // V of a step that some rows see and some do not, before the barrier that hands it over, by the threads that have brought it: what none
   // sees becomes zero (a weight of zero would not silence infinity or NaN), and the tile's flag says whether what is left is finite.
   const auto check_v = [&](int i, int ok, int buf) __attribute__((always_inline)) {
@@ -1033,7 +1050,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       rows_scores(sh.k[0], qf, n, hh, s0);
       rows_max<2>(s0, mx);
       mask_scores(tiles.tile(t_begin) * kBigTile, ok, s0, mx);
-      rows_settle(mx, at.scale, st);
+      settle(mx);
     }
     __syncthreads();                         // the first step replaces its K tile
     int i = t_begin;
@@ -1067,10 +1084,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         int ln = lane;
         if (FOUR) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
         // (past the last step: scores that are not used)
-        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st, [&] { return -(st.m_run == -INFINITY ? 0.f : st.m_run) * kLog2e - kBelow; });
+        if (far) {
+          const float ref = reference(st.m_run);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[k >> 4][k & 15] -= ref;
+        }
+        rows_step(sh.k[odd ^ 1], sh.v[odd], qf, s, nx, mx, at.scale, ln, st,
+                  [&] { return far ? -kBelow : -reference(st.m_run) * at.scale2 - kBelow; });
         if (i + 1 < t_end) {
           mask_scores(tiles.tile(i + 1) * kBigTile, ok, nx, mx);
-          rows_settle(mx, at.scale, st);
+          settle(mx);
         }
       }
       if constexpr (!FOUR) {
@@ -1091,7 +1114,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   static_assert(4 * 32 * 4 * kHeadDim <= 2 * sizeof(StepShared::k), "a wavefront's rows lie over the tiles");
   float l = st.l_run;
   l += __shfl_xor(l, 32);
-  const float m = part_max(st.m_run, l) * kLog2e;
+  const float m = part_max(st.m_run, l);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -1141,7 +1164,7 @@ __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv,
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (64 * k >= at.n_chunks) break;
-    const float f = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - top);
+    const float f = m[k] == -INFINITY ? 0.f : share(m[k], top, at.scale2);
     sum += f * l[k];
     for (int c0 = 0; c0 < 64 && 64 * k + c0 < at.n_chunks; c0 += 16) {
       // sixteen parts a time, four of them in each lane's hands: their reads are under way together (parts with no weight are not read)

@@ -171,9 +171,9 @@ __device__ __forceinline__ void rows_scores(const unsigned char* Ks, const bf16x
 // operand four slots ahead, and a few weights (scale and reference point in one fma, exp2, sum, packing), spread so
 // that a slot's vector work takes about as long as its products; the maxima of the new scores stand in the last
 // slots.  A weight is 2^(scale log2(e) score + reference()).  nx: the raw scores of the next step, mx: their maxima; s is used up.
-template <class M2>
+template <class Reference>
 __device__ __forceinline__ void rows_step(const unsigned char* Ks, const unsigned char* Vs, const bf16x8 (&qf)[8], f32x16 (&s)[2],
-                                          f32x16 (&nx)[2], float& mx, float scale, int lane, RowState& st, M2 reference) {
+                                          f32x16 (&nx)[2], float& mx, float scale, int lane, RowState& st, Reference reference) {
   constexpr float kLog2e = 1.4426950408889634f;
   constexpr int kAhead = 4;                                 // (6 and 8 measured the same)
   const int n = lane & 31, hh = lane >> 5;
@@ -248,7 +248,7 @@ __device__ __forceinline__ void rows_step(const unsigned char* Ks, const unsigne
   }
   __builtin_amdgcn_s_setprio(0);
 }
-// the same with the row's reference point as it is
+// the same for reference points of scaled scores
 __device__ __forceinline__ void rows_step(const unsigned char* Ks, const unsigned char* Vs, const bf16x8 (&qf)[8], f32x16 (&s)[2],
                                           f32x16 (&nx)[2], float& mx, float scale, int lane, RowState& st) {
   rows_step(Ks, Vs, qf, s, nx, mx, scale, lane, st, [&] { return -(st.m_run == -INFINITY ? 0.f : st.m_run) * 1.4426950408889634f; });

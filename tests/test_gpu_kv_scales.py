@@ -1,0 +1,66 @@
+"""tdk_kv_attend at scales of every size, and scores of every size."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kv_helpers as kh
+from paper_2604_03143_amd import tdk
+from test_gpu_kv import FORMATS, bf
+from test_gpu_kv_values import close, run
+
+pytestmark = pytest.mark.gpu
+
+
+def whole(b, fmt, H, group, seed, size=1.0):
+    """K and Q of small whole numbers (times `size`, a power of two): every score is exact in 32 bits."""
+    g = torch.Generator().manual_seed(seed)
+    k = bf(torch.randint(-3, 4, (b.pool_pages, b.T, H, 128), generator=g).double() * size)
+    v = bf(torch.randn(b.pool_pages, b.T, H, 128, generator=g))
+    q = bf(torch.randint(-3, 4, (b.n, H * group, 128), generator=g).double() * size)
+    if fmt == tdk.KV_BF16:
+        return k, v, q, k.double(), v.double()
+    packed = [kh.to4(x.float()) for x in (k, v)]
+    assert torch.equal(kh.from4(*packed[0]), k.double())                  # (whole numbers up to 3 are 4-bit values of any block they stand in)
+    return *(kh.pack4(*x, b.T) for x in packed), q, k.double(), kh.from4(*packed[1])
+
+
+SCALE_LENGTHS = pytest.mark.parametrize("lengths", [[(50, 1), (20, 3), (0, 1)], [(5000, 1)], [(0, 70), (90, 40)], [(2500, 9)], [(1500, 60)]])
+
+
+def check_scale(fmt, lengths, scale, size=1.0, kw={}, join=False):
+    H, group, T = 2, 4, 16
+    b = kh.Batch(lengths, T, 3)
+    dk, dv, q, k, v = whole(b, fmt, H, group, 5, size)
+    part = (None, None)
+    if join:
+        g = torch.Generator().manual_seed(6)
+        part = (torch.randn(b.n, H * group, 128, generator=g), torch.randn(b.n, H * group, generator=g))
+    want, wlse, mass, _ = kh.attend(b, k, v, q.double(), float(np.float32(scale)), **kw, part_out=None if part[0] is None else part[0].double(),
+                                    part_lse=None if part[1] is None else part[1].double())
+    got, glse = run(b, fmt, H, group, dk, dv, q, scale, **kw, part=part)
+    return want, wlse, mass, got, glse, max(h + n for h, n in lengths)
+
+
+@FORMATS
+@SCALE_LENGTHS
+@pytest.mark.parametrize("scale", [1.0e6, 1.0e8, 1.0e9, -1.0e9, 1.0e30, 2.0 ** 127])
+@pytest.mark.parametrize("kw,join", [({}, False), (dict(window=37, sink=5), True)])
+def test_large_scales(fmt, lengths, scale, kw, join):
+    """Only the largest scores of a row count, equally where several are equal.  Scores are whole numbers, exact; so are the weights then,
+    one and zero: the sums over n tokens add 2^-24 a step, the division one more, the output 2^-8.  The logarithm is the scaled maximum
+    (2^-24 of it; infinite where fp32 has no such number) plus that of a count (two steps of fp32)."""
+    want, wlse, mass, got, glse, n = check_scale(fmt, lengths, scale, kw=kw, join=join)
+    close(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -24 * (n + 4) * mass)
+    close(glse, wlse.float().double(), 2.0 ** -22 * (wlse.abs() + 16))
+
+
+@FORMATS
+@pytest.mark.parametrize("q_size", [2.0 ** 20, 2.0 ** 50])
+def test_large_scores_at_an_ordinary_scale(fmt, q_size):
+    """The same of queries and keys that are large themselves."""
+    for lengths in ([(50, 1), (20, 3), (0, 1)], [(5000, 1)], [(0, 70), (90, 40)]):
+        want, wlse, mass, got, glse, n = check_scale(fmt, lengths, 1 / math.sqrt(128), size=q_size)
+        close(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -24 * (n + 4) * mass)
+        close(glse, wlse, 2.0 ** -22 * (wlse.abs() + 16))
