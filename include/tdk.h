@@ -443,7 +443,8 @@ tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
  *              tokens, as tdk_attend_shared leaves it; out and lse are then those of both parts together
  *   workspace  tdk_kv_attend_workspace_bytes() bytes, 256-byte aligned, contents undefined; calls that may run at the same
  *              time (two streams, two graphs) need one each
- * Any finite scale is taken.  What a query does not see does not reach its result, whatever it holds (NaN and
+ * Any scale up to 2^127 in magnitude is taken, zero and denormal ones as they are (scores q . K beyond fp32 are infinite
+ * before they are scaled; a query all of whose scores are minus infinity counts as one that sees nothing).  What a query does not see does not reach its result, whatever it holds (NaN and
  * infinities included).  bf16 products with fp32 sums; the softmax weights are rounded to bf16 for the second product,
  * their sum is not.  Allocates nothing, one or two kernels, does not synchronise; results do not depend on what else runs. */
 typedef struct {

@@ -56,7 +56,7 @@ struct KvAttendDev {
   int32_t        piece_tiles;  // tiles of a part
   int32_t        n_rest;       // row blocks times parts
   int32_t        q_flip;       // the caller's scale was negative: the queries carry the sign
-  float          scale;        // its magnitude
+  float          scale;        // its magnitude, not zero
   float          scale2;       // times log2(e)
 };
 

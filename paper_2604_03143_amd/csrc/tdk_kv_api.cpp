@@ -2,6 +2,7 @@
 // Everything the host can see is checked before the device is asked for, so every refusal can be had without a GPU.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <memory>
 
 #include "tdk_errors.h"
@@ -24,6 +25,7 @@ constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;    // query rows of a call:
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1; // of one launch
 constexpr int32_t kMaxQHeads = 1 << 16;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;        // of a call, and of a sequence that a table has room for
+constexpr float   kMaxScale = 0x1p127f;                  // times log2(e) still an fp32 number
 constexpr int32_t kMaxSeqs = 1 << 30;                   // the search for a token's sequence counts in int32, in steps of 64
 
 bool off(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -245,6 +247,7 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     if (!a) return fail(TDK_ERR_INVALID_ARG, "attend io is NULL");
     KvAttendPlan p;
     if (!std::isfinite(a->scale)) return fail(TDK_ERR_INVALID_ARG, "scale must be finite");
+    if (std::fabs(a->scale) > kMaxScale) return fail(TDK_ERR_INVALID_ARG, "scale: a magnitude above 2^127");
     if (a->window < 0 || a->n_sink < 0) return fail(TDK_ERR_INVALID_ARG, "window / n_sink is negative");
     if (!attend_plan_kv(kv, batch, a->n_q_heads, a->window, a->n_sink, p))
       return fail(TDK_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of the KV heads");
@@ -284,9 +287,9 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     at.piece_tiles = p.piece_tiles;
     at.n_rest = (int32_t)(p.ids * p.n_chunks);
     at.q_flip = std::signbit(a->scale) ? 1 : 0;
-    // (a zero scale, uniform weights, becomes one so small that every scaled score rounds to zero: minus infinity stays what it is)
-    // (and one whose product with log2(e) would overflow the largest that does not: its scores are infinite all the same)
-    at.scale = std::fmin(std::fmax(std::fabs(a->scale), 1e-30f), 2.3e38f);
+    // (Zero, uniform weights, becomes the least number above it: what a row does not see stays minus infinity, and the scaled differences of all
+    // other scores are below 2^-20.)
+    at.scale = std::fmax(std::fabs(a->scale), std::numeric_limits<float>::denorm_min());
     at.scale2 = at.scale * 1.4426950408889634f;
     const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->format == TDK_KV_MXFP4, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_attend)");

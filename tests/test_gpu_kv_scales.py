@@ -64,3 +64,41 @@ def test_large_scores_at_an_ordinary_scale(fmt, q_size):
         want, wlse, mass, got, glse, n = check_scale(fmt, lengths, 1 / math.sqrt(128), size=q_size)
         close(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -24 * (n + 4) * mass)
         close(glse, wlse, 2.0 ** -22 * (wlse.abs() + 16))
+
+
+@FORMATS
+@SCALE_LENGTHS
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1.0e-45])
+def test_scales_that_make_all_weights_equal(fmt, lengths, scale):
+    """Scores of up to 2^122: times zero they are zero, times 2^-149 less than 2^-26 (the weights differ by less than a step of fp32)."""
+    want, wlse, mass, got, glse, n = check_scale(fmt, lengths, scale, size=2.0 ** 56)
+    close(got, want, 2.0 ** -8 * want.abs() + 2.0 ** -24 * (n + 6) * mass + 2.0 ** -8 * 2.0 ** -24)
+    close(glse, wlse, torch.full_like(wlse, 2.0 ** -22 * 16))
+
+
+@FORMATS
+@SCALE_LENGTHS
+@pytest.mark.parametrize("scale", [1.0e-36, -1.0e-36, 3.0e-37])
+def test_small_scales_of_large_scores(fmt, lengths, scale):
+    """Scales far below one are taken as they are: scores of up to 2^122 become ordinary ones.  Exact before the scale; the scale's and the
+    product's roundings are 2^-22 of an exponent of at most 64, and the weights are rounded to bf16 (2^-8)."""
+    want, wlse, mass, got, glse, n = check_scale(fmt, lengths, scale, size=2.0 ** 56)
+    e = 2.0 ** -22 * 64 + 2.0 ** -22 + 2.0 ** -24 * n
+    close(got, want, 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2 * e) * 1.01 * mass)
+    close(glse, wlse, torch.full_like(wlse, e + 2.0 ** -22 * 66))
+
+
+@pytest.mark.parametrize("lengths", [[(50, 1), (20, 3)], [(0, 70)], [(3000, 1)]])
+@pytest.mark.parametrize("scale", [0.0, 0.1, 1.0e30])
+def test_scores_that_are_all_minus_infinity(lengths, scale):
+    """Such a row is as one that sees nothing; joined, the other part is all there is."""
+    H, group, T = 2, 4, 16
+    b, g = kh.Batch(lengths, T, 3), torch.Generator().manual_seed(4)
+    k, v = torch.full((b.pool_pages, T, H, 128), -math.inf, dtype=torch.bfloat16), bf(torch.randn(b.pool_pages, T, H, 128, generator=g))
+    q = torch.ones(b.n, H * group, 128, dtype=torch.bfloat16)
+    out, lse = run(b, tdk.KV_BF16, H, group, k, v, q, scale)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    part = torch.randn(b.n, H * group, 128, generator=g), torch.randn(b.n, H * group, generator=g)
+    out, lse = run(b, tdk.KV_BF16, H, group, k, v, q, scale, part=part)
+    close(out, part[0].double(), 2.0 ** -8 * part[0].double().abs())
+    close(lse, part[1].double(), torch.zeros(()))

@@ -22,3 +22,8 @@ def test_too_many_sequences(n_seqs):
     for f in (lambda: tdk.tdk_kv_append(kv, cache(), batch(n_seqs=n_seqs), rows()), lambda: tdk.tdk_kv_read(kv, cache(), batch(n_seqs=n_seqs), rows()),
               lambda: tdk.tdk_kv_attend(kv, cache(), batch(n_seqs=n_seqs), io())):
         refused(f, tdk.ERR_UNSUPPORTED, "2^30 sequences")
+
+
+@pytest.mark.parametrize("scale", [1.01 * 2.0 ** 127, -3.4e38])
+def test_scales_whose_product_with_a_logarithm_is_beyond_fp32(scale):
+    refused(lambda: tdk.tdk_kv_attend(make(), cache(), batch(), io(scale=scale)), say="2^127")
