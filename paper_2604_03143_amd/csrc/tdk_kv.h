@@ -71,8 +71,9 @@ struct KvAttendPlan {
   size_t  o_part_ml = 0, bytes = 0;
 };
 
-hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st);
-hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st);
+// many: a call whose rows the caches would not hold for whoever comes next
+hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st);
+hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st);
 hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st);
 
 }  // namespace tdk

@@ -1208,17 +1208,17 @@ hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t
 
 }  // namespace
 
-// (one part per token: a call so large that the caches would hold nothing of it for whoever comes next; passed by, 12 500 tokens
-// 79 -> 74 us, 19 000 in 4 bits and back 132 -> 118)
-hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
-  auto kernel = rows.waves == 1 ? (four ? tdk_kv_append_kernel<true, true> : tdk_kv_append_kernel<false, true>)
-                                : (four ? tdk_kv_append_kernel<true, false> : tdk_kv_append_kernel<false, false>);
-  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, rows.waves == 1 && !four ? 256 : 64, st, kv, rows);
+// (many tokens pass the caches by: 12 500 tokens 79 -> 74 us, 19 000 in 4 bits and back 132 -> 118.  Few stay there, also where a wavefront has all of a
+// token: 250 tokens of four heads without queries, attention to 300 behind it, 38.5 -> 38.2 us together, 1500 tokens written 5.0 -> 4.2)
+hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st) {
+  auto kernel = many ? (four ? tdk_kv_append_kernel<true, true> : tdk_kv_append_kernel<false, true>)
+                     : (four ? tdk_kv_append_kernel<true, false> : tdk_kv_append_kernel<false, false>);
+  return launch(kernel, (int64_t)kv.n_tokens * rows.waves, many && !four ? 256 : 64, st, kv, rows);
 }
 
-hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, hipStream_t st) {
-  auto kernel = rows.waves == 1 ? (four ? tdk_kv_read_kernel<true, true> : tdk_kv_read_kernel<false, true>)
-                                : (four ? tdk_kv_read_kernel<true, false> : tdk_kv_read_kernel<false, false>);
+hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st) {
+  auto kernel = many ? (four ? tdk_kv_read_kernel<true, true> : tdk_kv_read_kernel<false, true>)
+                     : (four ? tdk_kv_read_kernel<true, false> : tdk_kv_read_kernel<false, false>);
   return launch(kernel, (int64_t)kv.n_tokens * rows.waves, 64, st, kv, rows);
 }
 

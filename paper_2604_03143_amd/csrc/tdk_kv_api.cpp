@@ -119,7 +119,8 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
   // A wavefront takes eight heads of a token at a time.  Few tokens: a workgroup for each eight heads, so that all of a call's
   // accesses are under way at once; many: the token's place and angles are found out once for all its heads.
   const int steps = (2 * kv->model.num_kv_heads + r.n_q_heads + 7) / 8;
-  r.waves = (int64_t)batch->n_tokens * steps <= (int64_t)8 * kv->n_cus ? steps : 1;
+  const bool many = (int64_t)batch->n_tokens * steps > (int64_t)8 * kv->n_cus;
+  r.waves = many ? 1 : steps;
   if ((int64_t)batch->n_tokens * r.waves * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
   std::copy(std::begin(kv->inv_freq), std::end(kv->inv_freq), std::begin(r.inv_freq));
   st = check_device(kv);
@@ -127,7 +128,7 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
   const KvDev d = kv_dev(kv, cache, batch);
   const bool four = kv->format == TDK_KV_MXFP4;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const hipError_t e = reading ? launch_kv_read(d, r, four, s) : launch_kv_append(d, r, four, s);
+  const hipError_t e = reading ? launch_kv_read(d, r, four, many, s) : launch_kv_append(d, r, four, many, s);
   return e == hipSuccess ? TDK_OK : hip_fail(e, reading ? "kernel launch (tdk_kv_read)" : "kernel launch (tdk_kv_append)");
 }
 
