@@ -102,3 +102,17 @@ def test_scores_that_are_all_minus_infinity(lengths, scale):
     out, lse = run(b, tdk.KV_BF16, H, group, k, v, q, scale, part=part)
     close(out, part[0].double(), 2.0 ** -8 * part[0].double().abs())
     close(lse, part[1].double(), torch.zeros(()))
+
+
+@FORMATS
+@SCALE_LENGTHS
+@pytest.mark.parametrize("scale", [8.0, 14.0, 20.0, -14.0])
+def test_reference_points_on_both_sides_of_two_to_the_twelfth(fmt, lengths, scale):
+    """Where the step kernel begins to subtract before it scales.  Scores are exact; a reference point of up to 2^12 in base 2 is rounded by 2^-12 at
+    most, twice (product and constant), and sums of two reference points meet: e = 2^-10 of an exponent, and as much for all other roundings.
+    (Where the largest weight meets a V of zero, what is left may be 1e-91: weights below 2^-126, the least normal fp32 number, with the 2^12 that
+    all are taken lower below 2^-114 of the largest, may vanish; 2^13 tokens of |V| up to 2^3 together no more than 2^-98.)"""
+    want, wlse, mass, got, glse, n = check_scale(fmt, lengths, scale)
+    e = 2.0 ** -9 + 2.0 ** -24 * n
+    close(got, want, 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2 * e) * 1.01 * mass + 2.0 ** -98)
+    close(glse, wlse, e + 2.0 ** -22 * wlse.abs())
