@@ -128,7 +128,7 @@ __device__ __forceinline__ u32x4 from4(uint32_t w, uint32_t e) {
 // 64 + 8 c .. + 7 of head 8 step + hl of the list K heads, Q heads, V heads: both halves of every pair of either style.
 // Every lane evaluates one of the 64 angles in double and passes cosine and sine (rounded to fp32 once) on through LDS: the bits of the rounds'
 // tables for any position, with no table to build or read, and no slower for it (12 500 tokens, a wavefront each: 79.3 us, with no angles at all 79.0).
-// What bounds it: many tokens, the row writes (12 500 tokens with 40 query heads: 391 MB in 68 us, 5.7 TB/s; the counters show no
+// What bounds it: many tokens, the row writes (12 500 tokens with 40 query heads: 391 MB in 69 us, 5.7 TB/s; the counters show no
 // byte more); few, its reads in a row: the starts, the length, the page number (4 tokens 3.7 us, 250 tokens 4.8).
 // ---------------------------------------------------------------------------------------------
 template <bool FOUR, bool ONCE>
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(ONCE && !FOUR ? 256 : 64) void tdk_kv_append_kernel
 }
 
 
-// Read: the same lanes, from the cache to rows (19 000 tokens out of 4 bits: 23 us, 4.4 TB/s, nearly all of it writes).
+// Read: the same lanes, from the cache to rows (19 000 tokens out of 4 bits 22 us, 4.4 TB/s, out of bf16 28 us, 5.4 TB/s; 64 tokens 4.7).
 template <bool FOUR, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_read_kernel(const KvDev kv, const KvRowsDev rows) {
   const int lane = threadIdx.x, c = lane & 7, hl = lane >> 3;
@@ -270,6 +270,8 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // Attention.  The query rows of a sequence and KV head are its (token, head of the group) pairs, tokens first; a workgroup takes a
 // block of them and a part of the tokens they see.  Scores are kept as the products leave them, unscaled.
+// The weights are rounded to bf16 for the second product (2^-8 of each at most): the matrix cores take both operands in one type, and V is bf16.  Their
+// sums, the scores and all that is joined stay in fp32.  Results differ from 64 bits by 0.0023 relative, from one rounding of the result by 0.0017.
 // ---------------------------------------------------------------------------------------------
 // A block of query rows: which sequence it belongs to, and what its rows see.
 struct Block {
@@ -612,8 +614,8 @@ __device__ __forceinline__ int rest_of(int heads, int& h) {
 // holds the scores of row n and tokens 16 tt + 4 g + i), V through LDS, where the transposing reads turn it.  With at most 16 of 128 rows to
 // share, a page read is used once: nothing is shared between the wavefronts, and none waits for another before the end.
 // What bounds it: the reads.  256 sequences of 4000 tokens, 5 heads per KV head: 6.3 TB/s (one KV head, rows in a run: 6.6), 64 of 16 000 6.2;
-// 250 of 2000 to 4200 tokens 511 us (6.1 TB/s; counters: matrix cores 4 %, vector units 8 % busy).  4 bits: 5.8 TB/s of pages, 6.2 with 32-token pages (vector units
-// 35 %); 32 rows of 64 sequences 61 us (4.7 TB/s), there the vector work of two row tiles.  Few sequences: the start (9 us for 4 of 257 tokens).
+// 250 of 2000 to 4200 tokens 511 us (6.1 TB/s; counters: matrix cores 4 %, vector units 9 % busy).  4 bits: 5.8 TB/s of pages, 6.2 with 32-token pages (vector units
+// 37 %); 32 rows of 64 sequences 61 us (4.7 TB/s), there the vector work of two row tiles.  Few sequences: the start (9 us for 4 of 257 tokens).
 template <bool FOUR, int NR>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR == 1 ? 3 : 2, FOUR && NR == 1 ? 3 : 2))) void tdk_kv_attend_rows_kernel(const KvDev kv, const KvAttendDev at) {
   constexpr int kJoin = kHeadDim + 4;        // floats per row of the joining area
@@ -817,8 +819,8 @@ namespace {
 // Many query rows (prompts): four wavefronts of 32 rows share 64-token steps of K and V in LDS (tdk_tiles.h): the score products of the next
 // step stand beside the weights and second products of this one, and the pages of the steps behind those travel to LDS meanwhile; 4-bit
 // pages by way of registers, where they become bf16.
-// What bounds it: the wait between a step's dependent stages, as in the spans' kernel.  Prompts of up to 2048 tokens behind 4000, 5 heads per KV head: 524 us, 845
-// TFLOP/s of what the queries see (counters: matrix cores 35 % busy, vector units 39 %, no bank conflicts; the order of unequal blocks loses a tenth).  Few of the
+// What bounds it: the wait between a step's dependent stages, as in the spans' kernel.  Prompts of up to 2048 tokens behind 4000, 5 heads per KV head: 519 us, 853
+// TFLOP/s of what the queries see (counters: matrix cores 35 % busy, vector units 39 %, no bank conflicts); in 4 bits 794 where bf16 has 815.  Few of the
 // 128 rows in use: the reads (64 sequences of 4000 tokens, 20 rows: 200 us, 5.3 TB/s); in 4 bits the way through registers (150 us, 1.9 TB/s).
 // ---------------------------------------------------------------------------------------------
 constexpr int kBlockRows = 4 * 32;
@@ -948,7 +950,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     return live;
   };
   // Scores of what the row does not see.  Each kind of border in a pass of its own, for the few steps that meet it: all of them together cost
-  // more than half a step (8192 tokens, a window of 1024: 281 -> 259 us, together with V checked where it is brought).
+  // more than half a step (8192 tokens, a window of 1024: 284 -> 257 us, together with V checked where it is brought; prompts without a window pay
+  // for the two, 519 -> 528 on the same card).
   const auto mask_scores = [&](int j0, int ok, f32x16 (&s)[2], float& mx) __attribute__((always_inline)) {
     const int j1 = j0 + kBigTile - 1;
     if (ok == 15 && all_see(at, w, j0, j1)) return;
@@ -1209,7 +1212,8 @@ hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t
 }  // namespace
 
 // (many tokens pass the caches by: 12 500 tokens 79 -> 74 us, 19 000 in 4 bits and back 132 -> 118.  Few stay there, also where a wavefront has all of a
-// token: 250 tokens of four heads without queries, attention to 300 behind it, 38.5 -> 38.2 us together, 1500 tokens written 5.0 -> 4.2)
+// token: 250 tokens of four heads without queries, attention to 300 tokens each behind it, 38.5 -> 38.2 us together; of 1500
+// tokens the append 5.0 -> 4.2, with attention 180 -> 185)
 hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st) {
   auto kernel = many ? (four ? tdk_kv_append_kernel<true, true> : tdk_kv_append_kernel<false, true>)
                      : (four ? tdk_kv_append_kernel<true, false> : tdk_kv_append_kernel<false, false>);

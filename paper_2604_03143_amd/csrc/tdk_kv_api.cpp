@@ -141,7 +141,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   many parts pay where there are few rounds (64 sequences of 16 000 tokens, one round 725 us, four 680; 66 of 4000 with 20 rows,
 //   one part 275, six 237), and not where there are many (250 of 4000: one part 512, two 529).
 //   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
-//   many (four prompts of 2048 tokens: one part 508 us, two 629).
+//   many (four prompts of up to 2048 tokens: one part 523 us, two 662).
 int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
   const bool four = kv->format == TDK_KV_MXFP4;
   const int64_t resident = (four && block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus;
