@@ -276,7 +276,8 @@ tdk_status tdk_check_layer(tdk_round* r, int32_t layer, const tdk_layer_io* io, 
  * weights rounded to bf16 for the second product); the listed pages go through the same products
  * from the payload.  The result agrees with the exact definition to about 1e-2 of the largest |V| at
  * scale = 1 / sqrt(128), in proportion for larger scales (not bit for bit).  Any finite scale is taken:
- * the kernels work with its magnitude and the query copies carry its sign; zero gives uniform weights. */
+ * the kernels work with its magnitude and the query copies carry its sign; zero (taken as 1e-30) gives uniform weights.
+ * Scaled scores have to stay below 2^24 in magnitude: the reference point of a row is rounded after scaling. */
 typedef struct {
   const void* q;
   int32_t     n_q;
@@ -444,9 +445,10 @@ tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
  *   workspace  tdk_kv_attend_workspace_bytes() bytes, 256-byte aligned, contents undefined; calls that may run at the same
  *              time (two streams, two graphs) need one each
  * Any scale up to 2^127 in magnitude is taken, zero and denormal ones as they are (scores q . K beyond fp32 are infinite
- * before they are scaled; a query all of whose scores are minus infinity counts as one that sees nothing).  What a query does not see does not reach its result, whatever it holds (NaN and
- * infinities included).  bf16 products with fp32 sums; the softmax weights are rounded to bf16 for the second product,
- * their sum is not.  Allocates nothing, one or two kernels, does not synchronise; results do not depend on what else runs. */
+ * before they are scaled; a query all of whose scores are minus infinity counts as one that sees nothing).  What a query
+ * does not see does not reach its result, whatever it holds (NaN and infinities included).  bf16 products with fp32 sums;
+ * the softmax weights are rounded to bf16 for the second product, their sum is not.  Allocates nothing, one or two
+ * kernels, does not synchronise; results do not depend on what else runs. */
 typedef struct {
   const void*    q;
   int64_t        q_stride;      /* elements, a multiple of 8, at least n_q_heads * D */

@@ -975,7 +975,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     rows_max<2>(s, mx);
   };
-  // The difference of score and reference point costs the step a twentieth (prompts 530 -> 545 us, with a window 259 -> 270), so it is taken where it is
+  // The difference of score and reference point costs the step 3 to 4 % (prompts 530 -> 545 us, with a window 259 -> 270), so it is taken where it is
   // needed: up to 2^12 the product of reference point and scale is rounded by 2^-12 at most, the same for all weights until the point moves.
   constexpr float kFar = 4096.f;
   bool far = false;                          // some row of the wavefront is beyond
