@@ -76,6 +76,31 @@ typedef struct {
   double  rope_theta;
 } tdk_model;
 
+/* How positions become angles beyond rope_theta alone.  A pair j < rotary_dim / 2 turns by f_j = theta^(-2 j / rotary_dim)
+ * radians per position; the elements behind rotary_dim pass as they are (half layout: pairs (j, j + rotary_dim / 2),
+ * interleaved: (2 j, 2 j + 1)).  For contexts `factor` times as long as the original_len tokens that a model was trained on:
+ *   LINEAR   every frequency is divided by factor
+ *   TURNS    by the turns r_j = original_len f_j / (2 pi) that a pair makes: those below `low` are divided by factor, those above
+ *            `high` stay, between them the share (r_j - low) / (high - low) of f_j stays and the rest is divided
+ *   INDEX    by the pair's number: with d(r) = rotary_dim ln(original_len / (2 pi r)) / (2 ln theta), the number of the pair that makes r
+ *            turns, the divided share grows from 0 at a = max(floor d(high), 0) to 1 at b = min(ceil d(low), rotary_dim - 1)
+ * magnitude: cosines and sines are multiplied by it (in double, before they are rounded to fp32).  Fields that a scaling does not use are
+ * not looked at.  Errors of the calls that take one: UNSUPPORTED (rotary_dim not a multiple of 16 from 16 to 128, unknown scaling),
+ * INVALID_ARG (magnitude outside [1e-6, 1e6], factor below 1, original_len not positive, not 0 < low < high; INDEX with theta <= 1). */
+#define TDK_ROPE_SCALE_NONE   0
+#define TDK_ROPE_SCALE_LINEAR 1
+#define TDK_ROPE_SCALE_TURNS  2
+#define TDK_ROPE_SCALE_INDEX  3
+typedef struct {
+  int32_t rotary_dim;
+  int32_t scaling;        /* TDK_ROPE_SCALE_* */
+  double  factor;
+  double  original_len;
+  double  low;
+  double  high;
+  double  magnitude;
+} tdk_rope;
+
 /* One shared span = one master. */
 typedef struct {
   int32_t span_tokens;    /* S >= 0 */
@@ -125,6 +150,12 @@ tdk_status tdk_round_create(const tdk_model* model,
                             const tdk_session* sessions, int32_t n_sessions,
                             const tdk_agent* agents, int32_t n_agents,
                             tdk_round** out);
+/* The same for caches whose keys were rotated by `rope` (tdk_kv_create_rope): re-rotation goes by its frequencies.  The cached keys carry the
+ * magnitude already.  Whole heads only: rotary_dim other than 128 is UNSUPPORTED. */
+tdk_status tdk_round_create_rope(const tdk_model* model, const tdk_rope* rope,
+                                 const tdk_session* sessions, int32_t n_sessions,
+                                 const tdk_agent* agents, int32_t n_agents,
+                                 tdk_round** out);
 void       tdk_round_destroy(tdk_round* r);             /* NULL-safe */
 size_t     tdk_scratch_bytes(const tdk_round* r);       /* device bytes the round owns */
 
@@ -357,8 +388,11 @@ tdk_status tdk_restore_layers(tdk_round* r, int32_t first_layer, int32_t n_layer
  * the masters of the next round (tdk_kv_read).  One call covers a batch of sequences of any lengths; all of a
  * batch's description lies on the device, so a captured call serves every later step of the same sizes.
  *
- * A cache has one of two formats:
+ * A cache has one of three formats:
  *   TDK_KV_BF16    planes [pool_pages][T][H][D] bf16: the pool of the rounds (tdk_layer_io.pool_k / pool_v)
+ *   TDK_KV_MXFP8   planes [pool_pages][H][T * 128 + T * 4] bytes, 1.94 times smaller: as MXFP4, but a value is a byte: one sign, four
+ *                  exponent bits (bias 7) and three mantissa bits, magnitudes up to 448; 0x7f and 0xff are NaN.  A block's byte
+ *                  255 makes all 32 NaN; values are infinite from 2^128 on (bytes from 247).
  *   TDK_KV_MXFP4   planes [pool_pages][H][T * 64 + T * 4] bytes, 3.8 times smaller: per page and KV head the 4-bit
  *                  values of its T tokens (64 bytes each, element 2 i in the low half of byte i), then the
  *                  block exponents (4 bytes each).  A value is one sign, two exponent bits and one mantissa bit
@@ -367,6 +401,7 @@ tdk_status tdk_restore_layers(tdk_round* r, int32_t first_layer, int32_t n_layer
  *                  infinite from 2^128 on (bytes 253 and 254). */
 #define TDK_KV_BF16  0
 #define TDK_KV_MXFP4 1
+#define TDK_KV_MXFP8 8
 
 typedef struct tdk_kv tdk_kv;   /* opaque, host memory only: geometry, format, rotation frequencies, device */
 
@@ -375,6 +410,8 @@ typedef struct tdk_kv tdk_kv;   /* opaque, host memory only: geometry, format, r
  * same time on several streams and from several threads.  Errors: INVALID_ARG, UNSUPPORTED (as
  * tdk_round_create; unknown format), NOMEM. */
 tdk_status tdk_kv_create(const tdk_model* model, int32_t format, tdk_kv** out);
+/* The same with positions that become angles by `rope`: tdk_kv_append and tdk_kv_rotate go by it. */
+tdk_status tdk_kv_create_rope(const tdk_model* model, const tdk_rope* rope, int32_t format, tdk_kv** out);
 void       tdk_kv_destroy(tdk_kv* kv);               /* NULL-safe; work that is enqueued already is not affected */
 size_t     tdk_kv_page_bytes(const tdk_kv* kv);      /* bytes of one page in one plane; 0 for NULL */
 
@@ -423,11 +460,33 @@ typedef struct {
  * arithmetic above, V as it is; with q, the rotated queries into q_out.  MXFP4: the fp32 values go to the nearest
  * 4-bit value of their block (ties to even); the block's power of two is 2^(floor(log2 m) - 2) of its largest
  * magnitude m, one higher from m = 1.75 * 2^n on (what lies beyond 6 becomes 6), and 2^-126 at least; a block with an
- * infinity or NaN becomes NaN, and in one with m from 1.75 * 2^127 on what rounds to 2^128 is infinite.  No two
+ * infinity or NaN becomes NaN, and in one with m from 1.75 * 2^127 on what rounds to 2^128 is infinite.  MXFP8: the same with
+ * 2^(floor(log2 m) - 8), one higher above 1.8125 * 2^n (what lies up to there becomes 448), and 2^-124 at least; in a block
+ * with m above 1.8125 * 2^127 what rounds to 2^128 is infinite.  No two
  * tokens of a batch may have the same place in the cache (sequences that share pages differ in the pages they
  * append to).  One kernel. */
 tdk_status tdk_kv_append(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
                          const tdk_kv_rows* rows, void* hip_stream);
+
+/* Rows that are rotated and stay rows: the batch's keys on their way to tdk_prompt_attend, queries, or, with `back`, keys out of a cache
+ * turned back to no position (the inverse: cosines and sines divided by the magnitude, the other way round).  Positions, starts and rows as in
+ * tdk_kv_append; max_len, block_table and table_stride of the batch are not looked at, and rows of no sequence or with a negative position are left
+ * alone.  Either plane may be NULL; out may be the source itself, with the same stride, and overlaps it nowhere else.  The handle's format does
+ * not matter.  One kernel. */
+typedef struct {
+  const void* k;                /* rows [H][D] */
+  int64_t     k_stride;
+  void*       k_out;
+  int64_t     k_out_stride;
+  const void* q;                /* rows [n_q_heads][D] */
+  int64_t     q_stride;
+  int32_t     n_q_heads;
+  void*       q_out;
+  int64_t     q_out_stride;
+  int32_t     back;
+} tdk_kv_rotate_io;
+
+tdk_status tdk_kv_rotate(const tdk_kv* kv, const tdk_kv_batch* batch, const tdk_kv_rotate_io* io, void* hip_stream);
 
 /* The inverse: the batch's tokens out of the cache into rows->k / rows->v (the same rows that append would take;
  * K stays rotated; 4-bit values as above).  rows->q must be NULL.  One kernel. */

@@ -296,7 +296,7 @@ struct RoundDeleter {
 };
 
 tdk_status round_create(const tdk_model* model, const tdk_session* sessions, int32_t n_sessions,
-                        const tdk_agent* agents, int32_t n_agents, tdk_round** out) {
+                        const tdk_agent* agents, int32_t n_agents, tdk_round** out, const tdk_rope* rope = nullptr) {
   if (!out) return fail(TDK_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
   tdk_status st = TDK_OK;
@@ -307,7 +307,7 @@ tdk_status round_create(const tdk_model* model, const tdk_session* sessions, int
   RoundPlan p;
   {
     std::string err;
-    const tdk_status ps = plan_round(model, sessions, n_sessions, agents, n_agents, p, err);
+    const tdk_status ps = plan_round(model, sessions, n_sessions, agents, n_agents, p, err, rope);
     if (ps != TDK_OK) return fail(ps, err);
   }
   r->sessions = p.sessions;
@@ -491,6 +491,15 @@ extern "C" {
 tdk_status tdk_round_create(const tdk_model* model, const tdk_session* sessions, int32_t n_sessions,
                             const tdk_agent* agents, int32_t n_agents, tdk_round** out) {
   return guarded([&] { return round_create(model, sessions, n_sessions, agents, n_agents, out); });
+}
+
+tdk_status tdk_round_create_rope(const tdk_model* model, const tdk_rope* rope, const tdk_session* sessions, int32_t n_sessions,
+                                 const tdk_agent* agents, int32_t n_agents, tdk_round** out) {
+  return guarded([&]() -> tdk_status {
+    if (out) *out = nullptr;
+    if (!rope) return fail(TDK_ERR_INVALID_ARG, "rope is NULL");
+    return round_create(model, sessions, n_sessions, agents, n_agents, out, rope);
+  });
 }
 
 void tdk_round_destroy(tdk_round* r) {

@@ -26,6 +26,9 @@ struct KvDev {
   int32_t        interleaved;
 };
 
+// The formats of pages.
+constexpr int kBf16 = 0, kMx4 = 4, kMx8 = 8;
+
 // Rows in and out of the cache.
 struct KvRowsDev {
   char*       k;
@@ -35,6 +38,22 @@ struct KvRowsDev {
   int64_t     k_stride, v_stride, q_stride, q_out_stride;   // bytes
   int32_t     n_q_heads;       // 0: no queries
   int32_t     waves;           // workgroups per token
+  double      inv_freq[kHalf];                              // of the pairs that turn, zero behind them
+  int32_t     rotary;          // elements of a head that turn
+  double      magnitude;       // of their cosines and sines
+};
+
+// Rows that are only rotated.
+struct KvRotateDev {
+  const char* k;               // NULL: none
+  const char* q;
+  char*       k_out;
+  char*       q_out;
+  int64_t     k_stride, k_out_stride, q_stride, q_out_stride;   // bytes
+  int32_t     n_k_heads, n_q_heads;                         // 0: none
+  int32_t     waves;           // workgroups per token
+  int32_t     rotary;
+  double      cos_size, sin_size;                           // factors of the cosines and sines
   double      inv_freq[kHalf];
 };
 
@@ -72,8 +91,13 @@ struct KvAttendPlan {
 };
 
 // many: a call whose rows the caches would not hold for whoever comes next
-hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st);
-hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, bool four, bool many, hipStream_t st);
-hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, bool four, hipStream_t st);
+hipError_t launch_kv_append(const KvDev& kv, const KvRowsDev& rows, int fmt, bool many, hipStream_t st);
+hipError_t launch_kv_append_rope(const KvDev& kv, const KvRowsDev& rows, int fmt, bool many, hipStream_t st);
+hipError_t launch_kv_rotate(const KvDev& kv, const KvRotateDev& r, bool many, hipStream_t st);
+hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, int fmt, bool many, hipStream_t st);
+hipError_t launch_kv8_read(const KvDev& kv, const KvRowsDev& rows, bool many, hipStream_t st);
+hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, int fmt, hipStream_t st);
+hipError_t launch_kv8_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, int64_t blocks, hipStream_t st);
+hipError_t launch_kv_join(const KvDev& kv, const KvAttendDev& at, int64_t rows, hipStream_t st);
 
 }  // namespace tdk

@@ -13,9 +13,11 @@ using namespace tdk;
 
 struct tdk_kv {
   tdk_model model{};
-  int32_t   format = TDK_KV_BF16;
+  int       fmt = kBf16;          // as the kernels have it: kBf16, kMx4, kMx8
   int       device = -1;          // -1: created where no device is
   int32_t   n_cus = 256;
+  int32_t   rotary = kHeadDim;
+  double    magnitude = 1.0;
   double    inv_freq[kHalf];
 };
 
@@ -97,6 +99,11 @@ tdk_status check_rows(const tdk_kv* kv, const tdk_kv_rows* r, bool reading) {
   return TDK_OK;
 }
 
+// Few tokens: a workgroup for each eight heads, so that all of a call's accesses are under way at once; many: the token's place and angles are
+// found out once for all its heads.
+int rows_steps(int heads) { return (heads + 7) / 8; }
+bool many_rows(const tdk_kv* kv, const tdk_kv_batch* b, int steps) { return (int64_t)b->n_tokens * steps > (int64_t)8 * kv->n_cus; }
+
 tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch, const tdk_kv_rows* rows, bool reading,
                      void* hip_stream) {
   bool nothing = false;
@@ -116,20 +123,80 @@ tdk_status move_rows(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_b
     r.q_out_stride = 2 * rows->q_out_stride;
     r.n_q_heads = rows->n_q_heads;
   }
-  // A wavefront takes eight heads of a token at a time.  Few tokens: a workgroup for each eight heads, so that all of a call's
-  // accesses are under way at once; many: the token's place and angles are found out once for all its heads.
-  const int steps = (2 * kv->model.num_kv_heads + r.n_q_heads + 7) / 8;
-  const bool many = (int64_t)batch->n_tokens * steps > (int64_t)8 * kv->n_cus;
+  const int steps = rows_steps(2 * kv->model.num_kv_heads + r.n_q_heads);
+  const bool many = many_rows(kv, batch, steps);
   r.waves = many ? 1 : steps;
   if ((int64_t)batch->n_tokens * r.waves * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
   std::copy(std::begin(kv->inv_freq), std::end(kv->inv_freq), std::begin(r.inv_freq));
+  r.rotary = kv->rotary;
+  r.magnitude = kv->magnitude;
   st = check_device(kv);
   if (st != TDK_OK || nothing) return st;
   const KvDev d = kv_dev(kv, cache, batch);
-  const bool four = kv->format == TDK_KV_MXFP4;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const hipError_t e = reading ? launch_kv_read(d, r, four, many, s) : launch_kv_append(d, r, four, many, s);
+  const hipError_t e = reading ? launch_kv_read(d, r, kv->fmt, many, s) : launch_kv_append(d, r, kv->fmt, many, s);
   return e == hipSuccess ? TDK_OK : hip_fail(e, reading ? "kernel launch (tdk_kv_read)" : "kernel launch (tdk_kv_append)");
+}
+
+// a plane of rows that are rotated: source and destination
+tdk_status check_rotated(const void* x, int64_t stride, const void* out, int64_t out_stride, int64_t row, const char* what) {
+  const std::string name(what);
+  if (!x != !out) return fail(TDK_ERR_INVALID_ARG, "rotate io: " + name + " and " + name + "_out come together");
+  if (!x) return TDK_OK;
+  if (off(x, 16) || off(out, 16)) return fail(TDK_ERR_INVALID_ARG, "rotate io: " + name + " / " + name + "_out must be 16-byte aligned");
+  if (bad_stride(stride, row) || bad_stride(out_stride, row))
+    return fail(TDK_ERR_INVALID_ARG, "rotate io: strides must be multiples of 8, at least the heads * 128");
+  if (x == out && stride != out_stride) return fail(TDK_ERR_INVALID_ARG, "rotate io: rows rotated in place keep their stride");
+  return TDK_OK;
+}
+
+tdk_status rotate_rows(const tdk_kv* kv, const tdk_kv_batch* b, const tdk_kv_rotate_io* a, void* hip_stream) {
+  if (!kv) return fail(TDK_ERR_INVALID_ARG, "kv handle is NULL");
+  if (!b || !a) return fail(TDK_ERR_INVALID_ARG, "batch / rotate io is NULL");
+  if (b->n_seqs < 0 || b->n_tokens < 0) return fail(TDK_ERR_INVALID_ARG, "batch: negative size");
+  if (b->n_tokens > kMaxTokens) return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 tokens");
+  if (b->n_seqs > kMaxSeqs) return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 sequences");
+  if (a->q && (a->n_q_heads < 1 || a->n_q_heads > kMaxQHeads)) return fail(TDK_ERR_INVALID_ARG, "rotate io: n_q_heads out of range");
+  tdk_status st = check_rotated(a->k, a->k_stride, a->k_out, a->k_out_stride, (int64_t)kv->model.num_kv_heads * kHeadDim, "k");
+  if (st == TDK_OK) st = check_rotated(a->q, a->q_stride, a->q_out, a->q_out_stride, (int64_t)a->n_q_heads * kHeadDim, "q");
+  if (st != TDK_OK) return st;
+  const bool nothing = b->n_seqs == 0 || b->n_tokens == 0 || (!a->k && !a->q);
+  if (!nothing && (!b->q_start || !b->seq_len)) return fail(TDK_ERR_INVALID_ARG, "batch: q_start / seq_len is NULL");
+  if (off(b->q_start, 4) || off(b->seq_len, 4)) return fail(TDK_ERR_INVALID_ARG, "batch: arrays must be 4-byte aligned");
+  KvRotateDev r{};
+  if (a->k) {
+    r.k = static_cast<const char*>(a->k);
+    r.k_out = static_cast<char*>(a->k_out);
+    r.k_stride = 2 * a->k_stride;
+    r.k_out_stride = 2 * a->k_out_stride;
+    r.n_k_heads = kv->model.num_kv_heads;
+  }
+  if (a->q) {
+    r.q = static_cast<const char*>(a->q);
+    r.q_out = static_cast<char*>(a->q_out);
+    r.q_stride = 2 * a->q_stride;
+    r.q_out_stride = 2 * a->q_out_stride;
+    r.n_q_heads = a->n_q_heads;
+  }
+  const int steps = rows_steps(r.n_k_heads + r.n_q_heads);
+  const bool many = many_rows(kv, b, steps);
+  r.waves = many ? 1 : steps;
+  if ((int64_t)b->n_tokens * r.waves * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
+  r.rotary = kv->rotary;
+  r.cos_size = a->back ? 1.0 / kv->magnitude : kv->magnitude;
+  r.sin_size = a->back ? -r.cos_size : r.cos_size;
+  std::copy(std::begin(kv->inv_freq), std::end(kv->inv_freq), std::begin(r.inv_freq));
+  st = check_device(kv);
+  if (st != TDK_OK || nothing) return st;
+  KvDev d{};
+  d.q_start = b->q_start;
+  d.seq_len = b->seq_len;
+  d.n_seqs = b->n_seqs;
+  d.n_tokens = b->n_tokens;
+  d.page_shift = 4;
+  d.interleaved = kv->model.rope_style == TDK_ROPE_INTERLEAVED;
+  const hipError_t e = launch_kv_rotate(d, r, many, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_rotate)");
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -143,7 +210,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
 //   many (four prompts of up to 2048 tokens: one part 523 us, two 662).
 int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
-  const bool four = kv->format == TDK_KV_MXFP4;
+  const bool four = kv->fmt == kMx4;
   const int64_t resident = (four && block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus;
   const int64_t most = std::min<int64_t>((len + 255) / 256, 256);
   if (per_seq > 128 || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
@@ -157,6 +224,33 @@ int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_
     if (rounds > 16) break;
   }
   return best;
+}
+
+tdk_status kv_create(const tdk_model* model, const tdk_rope* rope, int32_t format, tdk_kv** out) {
+  if (!out) return fail(TDK_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  std::string err;
+  tdk_status st = plan_check_model(model, err);
+  if (st == TDK_OK && rope) st = plan_check_rope(model, rope, err);
+  if (st != TDK_OK) return fail(st, err);
+  if (format != TDK_KV_BF16 && format != TDK_KV_MXFP4 && format != TDK_KV_MXFP8) return fail(TDK_ERR_UNSUPPORTED, "unknown cache format");
+  auto kv = std::make_unique<tdk_kv>();
+  kv->model = *model;
+  kv->fmt = format == TDK_KV_MXFP8 ? kMx8 : format == TDK_KV_MXFP4 ? kMx4 : kBf16;
+  rope_frequencies(model, rope, kv->inv_freq);
+  if (rope) {
+    kv->rotary = rope->rotary_dim;
+    kv->magnitude = rope->magnitude;
+  }
+  int dev = -1, cus = 0;
+  if (hipGetDevice(&dev) == hipSuccess) {
+    kv->device = dev;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0) kv->n_cus = cus;
+  } else {
+    (void)hipGetLastError();
+  }
+  *out = kv.release();
+  return TDK_OK;
 }
 
 // window, n_sink: as in the call; without a window the plan is the one with the most parts.  false: bad arguments
@@ -175,7 +269,7 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   // in LDS; a few of its rows already read at the memory's rate in bf16 (64 sequences of 4000 tokens, 20 rows: 200 us, two passes of 16 rows
   // over the pages 290).  In 4 bits its tiles come by way of registers, one step ahead of another, and the rows kernel with 32 rows is ahead
   // up to two blocks (20 rows 61 us against 165; 64 rows 130 against 150; few sequences with 40 to 50 rows are up to 12 % behind).
-  p.block_rows = rows <= 16 ? 16 : rows <= 64 && kv->format == TDK_KV_MXFP4 ? 32 : 128;
+  p.block_rows = rows <= 16 ? 16 : rows <= 64 && kv->fmt == kMx4 ? 32 : 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // tokens that a block sees: all, or the window of its rows and the first tokens
@@ -197,34 +291,25 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
 extern "C" {
 
 tdk_status tdk_kv_create(const tdk_model* model, int32_t format, tdk_kv** out) {
+  return guarded([&] { return kv_create(model, nullptr, format, out); });
+}
+
+tdk_status tdk_kv_create_rope(const tdk_model* model, const tdk_rope* rope, int32_t format, tdk_kv** out) {
   return guarded([&]() -> tdk_status {
-    if (!out) return fail(TDK_ERR_INVALID_ARG, "out is NULL");
-    *out = nullptr;
-    std::string err;
-    const tdk_status st = plan_check_model(model, err);
-    if (st != TDK_OK) return fail(st, err);
-    if (format != TDK_KV_BF16 && format != TDK_KV_MXFP4) return fail(TDK_ERR_UNSUPPORTED, "unknown cache format");
-    auto kv = std::make_unique<tdk_kv>();
-    kv->model = *model;
-    kv->format = format;
-    for (int j = 0; j < kHalf; ++j) kv->inv_freq[j] = std::pow(model->rope_theta, -(double)(2 * j) / (double)kHeadDim);
-    int dev = -1, cus = 0;
-    if (hipGetDevice(&dev) == hipSuccess) {
-      kv->device = dev;
-      if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0) kv->n_cus = cus;
-    } else {
-      (void)hipGetLastError();
-    }
-    *out = kv.release();
-    return TDK_OK;
+    if (out) *out = nullptr;
+    return rope ? kv_create(model, rope, format, out) : fail(TDK_ERR_INVALID_ARG, "rope is NULL");
   });
+}
+
+tdk_status tdk_kv_rotate(const tdk_kv* kv, const tdk_kv_batch* batch, const tdk_kv_rotate_io* io, void* hip_stream) {
+  return guarded([&] { return rotate_rows(kv, batch, io, hip_stream); });
 }
 
 void tdk_kv_destroy(tdk_kv* kv) { delete kv; }
 
 size_t tdk_kv_page_bytes(const tdk_kv* kv) {
   if (!kv) return 0;
-  return (size_t)kv->model.page_tokens * kv->model.num_kv_heads * (kv->format == TDK_KV_MXFP4 ? 68 : 256);
+  return (size_t)kv->model.page_tokens * kv->model.num_kv_heads * (kv->fmt == kMx4 ? 68 : kv->fmt == kMx8 ? 132 : 256);
 }
 
 tdk_status tdk_kv_append(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch, const tdk_kv_rows* rows, void* hip_stream) {
@@ -292,7 +377,7 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     // other scores are below 2^-20.)
     at.scale = std::fmax(std::fabs(a->scale), std::numeric_limits<float>::denorm_min());
     at.scale2 = at.scale * 1.4426950408889634f;
-    const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->format == TDK_KV_MXFP4, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->fmt, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_attend)");
   });
 }

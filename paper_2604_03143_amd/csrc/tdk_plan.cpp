@@ -24,13 +24,59 @@ tdk_status plan_check_model(const tdk_model* m, std::string& err) {
   return TDK_OK;
 }
 
+tdk_status plan_check_rope(const tdk_model* m, const tdk_rope* r, std::string& err) {
+  auto refuse = [&](tdk_status st, const char* msg) { err = msg; return st; };
+  if (!r) return refuse(TDK_ERR_INVALID_ARG, "rope is NULL");
+  if (r->rotary_dim < 16 || r->rotary_dim > kHeadDim || r->rotary_dim % 16)
+    return refuse(TDK_ERR_UNSUPPORTED, "rope: rotary_dim must be a multiple of 16 from 16 to 128");
+  if (r->scaling < TDK_ROPE_SCALE_NONE || r->scaling > TDK_ROPE_SCALE_INDEX) return refuse(TDK_ERR_UNSUPPORTED, "rope: unknown scaling");
+  if (!(r->magnitude >= 1e-6 && r->magnitude <= 1e6)) return refuse(TDK_ERR_INVALID_ARG, "rope: magnitude must lie in [1e-6, 1e6]");
+  if (r->scaling == TDK_ROPE_SCALE_NONE) return TDK_OK;
+  if (!(r->factor >= 1.0) || !std::isfinite(r->factor)) return refuse(TDK_ERR_INVALID_ARG, "rope: factor must be finite and at least 1");
+  if (r->scaling == TDK_ROPE_SCALE_LINEAR) return TDK_OK;
+  if (!(r->original_len > 0.0) || !std::isfinite(r->original_len)) return refuse(TDK_ERR_INVALID_ARG, "rope: original_len must be positive and finite");
+  if (!(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high))
+    return refuse(TDK_ERR_INVALID_ARG, "rope: low and high must be finite, 0 < low < high");
+  if (r->scaling == TDK_ROPE_SCALE_INDEX && !(m->rope_theta > 1.0))
+    return refuse(TDK_ERR_INVALID_ARG, "rope: numbers of pairs go by the logarithm of rope_theta, which must be above 1");
+  return TDK_OK;
+}
+
+void rope_frequencies(const tdk_model* m, const tdk_rope* r, double (&freq)[kHalf]) {
+  const int R = r ? r->rotary_dim : kHeadDim;
+  double first = 0, last = 0;                // TDK_ROPE_SCALE_INDEX: the pairs between which the change fades in
+  if (r && r->scaling == TDK_ROPE_SCALE_INDEX) {
+    // the number of the pair that makes so many turns over the original length
+    const auto pair_of = [&](double turns) { return R * std::log(r->original_len / (turns * 2.0 * M_PI)) / (2.0 * std::log(m->rope_theta)); };
+    first = std::max(std::floor(pair_of(r->high)), 0.0);
+    last = std::min(std::ceil(pair_of(r->low)), (double)(R - 1));
+  }
+  for (int j = 0; j < kHalf; ++j) {
+    if (j >= R / 2) { freq[j] = 0.0; continue; }
+    const double f = std::pow(m->rope_theta, -(double)(2 * j) / (double)R);
+    double keep = 1.0;                       // how much of the frequency stays as it is
+    if (r) switch (r->scaling) {
+      case TDK_ROPE_SCALE_LINEAR: keep = 0.0; break;
+      case TDK_ROPE_SCALE_TURNS: keep = std::min(std::max((r->original_len * f / (2.0 * M_PI) - r->low) / (r->high - r->low), 0.0), 1.0); break;
+      case TDK_ROPE_SCALE_INDEX: keep = 1.0 - std::min(std::max((j - first) / std::max(last - first, 0.001), 0.0), 1.0); break;
+      default: break;
+    }
+    freq[j] = keep == 1.0 ? f : f / r->factor * (1.0 - keep) + f * keep;
+  }
+}
 
 tdk_status plan_round(const tdk_model* model, const tdk_session* sessions, int32_t n_sessions,
-                      const tdk_agent* agents, int32_t n_agents, RoundPlan& out, std::string& err) {
+                      const tdk_agent* agents, int32_t n_agents, RoundPlan& out, std::string& err, const tdk_rope* rope) {
   auto refuse = [&](tdk_status st, const char* msg) { err = msg; return st; };
   out = RoundPlan();
   tdk_status st = plan_check_model(model, err);
   if (st != TDK_OK) return st;
+  if (rope) {
+    if ((st = plan_check_rope(model, rope, err)) != TDK_OK) return st;
+    if (rope->rotary_dim != kHeadDim) return refuse(TDK_ERR_UNSUPPORTED, "rope: the rounds turn whole heads");
+  }
+  double freq[kHalf];
+  rope_frequencies(model, rope, freq);
   if (n_sessions < 0 || n_agents < 0) return refuse(TDK_ERR_INVALID_ARG, "negative session or agent count");
   if ((n_sessions && !sessions) || (n_agents && !agents)) return refuse(TDK_ERR_INVALID_ARG, "sessions / agents is NULL");
   const int T = model->page_tokens;
@@ -135,23 +181,11 @@ tdk_status plan_round(const tdk_model* model, const tdk_session* sessions, int32
         out.seg_src.push_back(segs[q].src_tok);
         seg_moved |= segs[q].dst_pos != segs[q].diff_pos;
         const double delta = (double)(segs[q].dst_pos - (hs.master_pos0 + segs[q].src_tok));
-        for (int j = 0; j < kHalf; ++j) {
-          const double inv_freq = std::pow(model->rope_theta, -(double)(2 * j) / (double)model->head_dim);
-          out.segtab.push_back((float)std::cos(delta * inv_freq));
-        }
-        for (int j = 0; j < kHalf; ++j) {
-          const double inv_freq = std::pow(model->rope_theta, -(double)(2 * j) / (double)model->head_dim);
-          out.segtab.push_back((float)std::sin(delta * inv_freq));
-        }
+        for (int j = 0; j < kHalf; ++j) out.segtab.push_back((float)std::cos(delta * freq[j]));
+        for (int j = 0; j < kHalf; ++j) out.segtab.push_back((float)std::sin(delta * freq[j]));
         const double moved = (double)(segs[q].dst_pos - segs[q].diff_pos);
-        for (int j = 0; j < kHalf; ++j) {
-          const double inv_freq = std::pow(model->rope_theta, -(double)(2 * j) / (double)model->head_dim);
-          out.segtab_diff.push_back((float)std::cos(moved * inv_freq));
-        }
-        for (int j = 0; j < kHalf; ++j) {
-          const double inv_freq = std::pow(model->rope_theta, -(double)(2 * j) / (double)model->head_dim);
-          out.segtab_diff.push_back((float)std::sin(moved * inv_freq));
-        }
+        for (int j = 0; j < kHalf; ++j) out.segtab_diff.push_back((float)std::cos(moved * freq[j]));
+        for (int j = 0; j < kHalf; ++j) out.segtab_diff.push_back((float)std::sin(moved * freq[j]));
         for (int32_t m = segs[q].src_tok; m < segs[q].src_tok + segs[q].len; ++m) {
           const int64_t pos = segs[q].dst_pos + (m - segs[q].src_tok);
           out.rowmap.push_back((int32_t)((int64_t)a.block_table[pos / T] * T + pos % T));
@@ -186,8 +220,7 @@ tdk_status plan_round(const tdk_model* model, const tdk_session* sessions, int32
       float* c = tabs[which];
       float* sn = c + kHalf;
       for (int j = 0; j < kHalf; ++j) {
-        const double inv_freq = std::pow(model->rope_theta, -(double)(2 * j) / (double)model->head_dim);
-        const double phi = deltas[which] * inv_freq;
+        const double phi = deltas[which] * freq[j];
         c[j] = (float)std::cos(phi);
         sn[j] = (float)std::sin(phi);
       }

@@ -47,8 +47,12 @@ struct RoundPlan {
 
 // Every function returns TDK_OK or the status to hand to the caller, with the reason in `err`.
 tdk_status plan_check_model(const tdk_model* m, std::string& err);
+tdk_status plan_check_rope(const tdk_model* m, const tdk_rope* r, std::string& err);
+// rope NULL: rope_theta alone, all of the head
 tdk_status plan_round(const tdk_model* model, const tdk_session* sessions, int32_t n_sessions,
-                      const tdk_agent* agents, int32_t n_agents, RoundPlan& p, std::string& err);
+                      const tdk_agent* agents, int32_t n_agents, RoundPlan& p, std::string& err, const tdk_rope* rope = nullptr);
+// radians per position of the pairs; 0 for those that do not turn
+void rope_frequencies(const tdk_model* m, const tdk_rope* r, double (&freq)[kHalf]);
 
 // Work list for `group` agents per item in the order of a static launch (item i runs on XCD i % 8), and the same
 // items grouped by that XCD (queue x = queued[q_begin[x] .. q_begin[x + 1])).

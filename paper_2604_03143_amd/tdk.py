@@ -19,7 +19,8 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_HIP, ERR_NOMEM = range(6
 BF16 = 0
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 PLANE_K, PLANE_V = 1, 2
-KV_BF16, KV_MXFP4 = 0, 1
+KV_BF16, KV_MXFP4, KV_MXFP8 = 0, 1, 8
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_TURNS, ROPE_SCALE_INDEX = range(4)
 (KERNEL_REROTATE, KERNEL_FLAG, KERNEL_COMPACT, KERNEL_GATHER, KERNEL_DECODE, KERNEL_SCATTER,
  KERNEL_KEYDIFF, KERNEL_SELECT, KERNEL_MASTER, KERNEL_ATTEND_QROT, KERNEL_ATTEND_MASTER, KERNEL_ATTEND_DIFF,
  KERNEL_ATTEND_MERGE) = range(13)
@@ -32,12 +33,12 @@ STATIC_SCRATCH_BYTES = 4 << 20
 
 EXPORTS = (
     "tdk_status_str", "tdk_last_error", "tdk_version", "tdk_kernel_name",
-    "tdk_round_create", "tdk_round_destroy", "tdk_scratch_bytes", "tdk_round_tune", "tdk_round_agents_per_group",
+    "tdk_round_create", "tdk_round_create_rope", "tdk_round_destroy", "tdk_scratch_bytes", "tdk_round_tune", "tdk_round_agents_per_group",
     "tdk_rerotate_round", "tdk_diff_encode", "tdk_diff_encode_static", "tdk_diff_decode", "tdk_restore_layers", "tdk_check_layer",
     "tdk_diff_encode_plane", "tdk_diff_decode_plane", "tdk_attend_workspace_bytes", "tdk_attend_shared",
     "tdk_prompt_plan_create", "tdk_prompt_plan_destroy", "tdk_prompt_plan_n_sessions", "tdk_prompt_plan_span",
     "tdk_prompt_plan_session_of", "tdk_prompt_plan_segments",
-    "tdk_kv_create", "tdk_kv_destroy", "tdk_kv_page_bytes", "tdk_kv_append", "tdk_kv_read",
+    "tdk_kv_create", "tdk_kv_create_rope", "tdk_kv_destroy", "tdk_kv_page_bytes", "tdk_kv_append", "tdk_kv_read", "tdk_kv_rotate",
     "tdk_kv_attend_workspace_bytes", "tdk_kv_attend",
     "tdk_timing_enable", "tdk_timing_read", "tdk_timing_reset",
     "tdk_dense_bytes", "tdk_diff_bytes", "tdk_family_cost",
@@ -50,6 +51,11 @@ class Model(C.Structure):
     _fields_ = [("num_layers", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("page_tokens", C.c_int32), ("dtype", C.c_int32), ("rope_style", C.c_int32),
                 ("rope_theta", C.c_double)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("scaling", C.c_int32), ("factor", C.c_double), ("original_len", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
 
 
 class Session(C.Structure):
@@ -108,6 +114,11 @@ class KvRows(C.Structure):
                 ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("q_out", C.c_void_p), ("q_out_stride", C.c_int64)]
 
 
+class KvRotateIO(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("k_stride", C.c_int64), ("k_out", C.c_void_p), ("k_out_stride", C.c_int64), ("q", C.c_void_p),
+                ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("q_out", C.c_void_p), ("q_out_stride", C.c_int64), ("back", C.c_int32)]
+
+
 class KvAttendIO(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("scale", C.c_float), ("out", C.c_void_p),
                 ("out_stride", C.c_int64), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
@@ -142,6 +153,8 @@ def load() -> C.CDLL:
     L.tdk_kernel_name.argtypes = [C.c_int32]
     L.tdk_round_create.argtypes = [C.POINTER(Model), C.POINTER(Session), C.c_int32, C.POINTER(Agent),
                                    C.c_int32, C.POINTER(C.c_void_p)]
+    L.tdk_round_create_rope.argtypes = [C.POINTER(Model), C.POINTER(Rope), C.POINTER(Session), C.c_int32, C.POINTER(Agent),
+                                        C.c_int32, C.POINTER(C.c_void_p)]
     L.tdk_round_destroy.argtypes = [C.c_void_p]
     L.tdk_round_destroy.restype = None
     L.tdk_scratch_bytes.argtypes = [C.c_void_p]
@@ -169,6 +182,8 @@ def load() -> C.CDLL:
     L.tdk_restore_layers.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                      C.POINTER(LayerIO), C.POINTER(Diff), C.POINTER(PingPong), C.c_void_p, C.c_void_p]
     L.tdk_kv_create.argtypes = [C.POINTER(Model), C.c_int32, C.POINTER(C.c_void_p)]
+    L.tdk_kv_create_rope.argtypes = [C.POINTER(Model), C.POINTER(Rope), C.c_int32, C.POINTER(C.c_void_p)]
+    L.tdk_kv_rotate.argtypes = [C.c_void_p, C.POINTER(KvBatch), C.POINTER(KvRotateIO), C.c_void_p]
     L.tdk_kv_destroy.argtypes = [C.c_void_p]
     L.tdk_kv_destroy.restype = None
     L.tdk_kv_page_bytes.argtypes = [C.c_void_p]
@@ -235,6 +250,11 @@ def model(num_layers, num_kv_heads=8, head_dim=128, page_tokens=16, rope_theta=1
     return Model(num_layers, num_kv_heads, head_dim, page_tokens, dtype, rope_style, float(rope_theta))
 
 
+def rope(rotary_dim: int = 128, scaling: int = ROPE_SCALE_NONE, factor: float = 1.0, original_len: float = 0.0, low: float = 0.0,
+         high: float = 0.0, magnitude: float = 1.0) -> Rope:
+    return Rope(int(rotary_dim), int(scaling), float(factor), float(original_len), float(low), float(high), float(magnitude))
+
+
 class Round:
     """Owns a tdk_round handle."""
 
@@ -263,6 +283,18 @@ def tdk_round_create(mdl: Model, span_tokens: Sequence[int], master_pos0: Sequen
     """segments: per agent an int array [n_seg, 3] of (src_tok, dst_pos, len), empty = identity layout.
     segment_diff_pos: per agent the position of each segment when the diff to restore was encoded
     (default: dst_pos, a diff of this round)."""
+    return _round_create(mdl, None, span_tokens, master_pos0, agent_session, agent_pos0, block_tables, agent_diff_pos0, segments, segment_diff_pos)
+
+
+def tdk_round_create_rope(mdl: Model, rp: Rope, span_tokens: Sequence[int], master_pos0: Sequence[int],
+                          agent_session: Sequence[int], agent_pos0: Sequence[int],
+                          block_tables: Sequence[np.ndarray], agent_diff_pos0: Optional[Sequence[int]] = None,
+                          segments: Optional[Sequence[np.ndarray]] = None,
+                          segment_diff_pos: Optional[Sequence[np.ndarray]] = None) -> Round:
+    return _round_create(mdl, rp, span_tokens, master_pos0, agent_session, agent_pos0, block_tables, agent_diff_pos0, segments, segment_diff_pos)
+
+
+def _round_create(mdl, rp, span_tokens, master_pos0, agent_session, agent_pos0, block_tables, agent_diff_pos0, segments, segment_diff_pos) -> Round:
     ns, na = len(span_tokens), len(agent_session)
     sess = (Session * max(ns, 1))()
     for s in range(ns):
@@ -284,7 +316,10 @@ def tdk_round_create(mdl: Model, span_tokens: Sequence[int], master_pos0: Sequen
             nseg, segp = len(segments[i]), C.cast(sg, C.c_void_p)
         ags[i] = Agent(int(agent_session[i]), int(agent_pos0[i]), bt.ctypes.data, len(bt), dp, nseg, segp)
     out = C.c_void_p()
-    _check(load().tdk_round_create(C.byref(mdl), sess, ns, ags, na, C.byref(out)), "tdk_round_create")
+    if rp is None:
+        _check(load().tdk_round_create(C.byref(mdl), sess, ns, ags, na, C.byref(out)), "tdk_round_create")
+    else:
+        _check(load().tdk_round_create_rope(C.byref(mdl), C.byref(rp), sess, ns, ags, na, C.byref(out)), "tdk_round_create_rope")
     return Round(out.value, na, None)
 
 
@@ -440,6 +475,12 @@ def tdk_kv_create(mdl: Model, fmt: int = KV_BF16) -> Kv:
     return Kv(out.value)
 
 
+def tdk_kv_create_rope(mdl: Model, rp: Rope, fmt: int = KV_BF16) -> Kv:
+    out = C.c_void_p()
+    _check(load().tdk_kv_create_rope(C.byref(mdl), C.byref(rp), int(fmt), C.byref(out)), "tdk_kv_create_rope")
+    return Kv(out.value)
+
+
 def tdk_kv_destroy(kv: Kv) -> None:
     kv.destroy()
 
@@ -468,6 +509,16 @@ def tdk_kv_append(kv: Kv, cache: KvCache, batch: KvBatch, rows: KvRows, stream: 
 
 def tdk_kv_read(kv: Kv, cache: KvCache, batch: KvBatch, rows: KvRows, stream: int = 0) -> None:
     _check(load().tdk_kv_read(kv.handle, C.byref(cache), C.byref(batch), C.byref(rows), C.c_void_p(stream)), "tdk_kv_read")
+
+
+def kv_rotate_io(k, k_stride: int, k_out, k_out_stride: int, q=None, q_stride: int = 0, n_q_heads: int = 0, q_out=None, q_out_stride: int = 0,
+                 back: bool = False) -> KvRotateIO:
+    return KvRotateIO(_ptr(k), int(k_stride), _ptr(k_out), int(k_out_stride), _ptr(q), int(q_stride), int(n_q_heads), _ptr(q_out),
+                      int(q_out_stride), int(bool(back)))
+
+
+def tdk_kv_rotate(kv: Kv, batch: KvBatch, io: KvRotateIO, stream: int = 0) -> None:
+    _check(load().tdk_kv_rotate(kv.handle, C.byref(batch), C.byref(io), C.c_void_p(stream)), "tdk_kv_rotate")
 
 
 def kv_attend_io(q, q_stride: int, n_q_heads: int, scale: float, out, out_stride: int, lse, workspace, workspace_bytes: int,
