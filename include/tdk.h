@@ -530,6 +530,52 @@ size_t     tdk_kv_attend_workspace_bytes(const tdk_kv* kv, const tdk_kv_batch* b
 tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv_batch* batch,
                          const tdk_kv_attend_io* a, void* hip_stream);
 
+/* Attention of prompts that are not in pages: packed sequences, keys and values straight from the projections (rotated by
+ * tdk_kv_rotate).  Sequence s has the keys k_start[s] .. k_start[s + 1] - 1 of the rows k and v, and the queries q_start[s] .. q_start[s + 1] - 1;
+ * its queries are its last tokens: query t of n sees key j iff j <= p = n_keys - n + t, and window = 0 or j > p - window or j < n_sink.  Queries of
+ * a sequence with fewer keys than queries that come before the first key see nothing.  A prompt's first pass has as many queries as
+ * keys (both arrays may be one); a later chunk has all keys so far.  Starts must not decrease and are cut to [0, n_q] and [0, n_k];
+ * queries of no sequence are left alone.
+ *   n_q, n_k     rows of q and out, rows of k and v
+ *   max_len      keys of the longest sequence that is expected, as in tdk_kv_batch
+ * The handle gives the heads and the device; its format and frequencies do not matter. */
+typedef struct {
+  int32_t        n_seqs;
+  int32_t        n_q;
+  int32_t        n_k;
+  int32_t        max_len;
+  const int32_t* q_start;       /* DEV [n_seqs + 1] */
+  const int32_t* k_start;       /* DEV [n_seqs + 1] */
+} tdk_prompt_batch;
+
+/* As tdk_kv_attend_io, with rows k and v of [H][D] bf16 (strides at most 2^24 elements).  out_f32: out is fp32 (out_stride in elements of
+ * it), so that it can be another call's part_out: a prompt attends to its own rows here and to its history in the pages with
+ * tdk_kv_attend, whose hole is the prompt's span. */
+typedef struct {
+  const void*    q;
+  int64_t        q_stride;
+  int32_t        n_q_heads;
+  const void*    k;
+  int64_t        k_stride;
+  const void*    v;
+  int64_t        v_stride;
+  float          scale;
+  void*          out;
+  int64_t        out_stride;
+  int32_t        out_f32;
+  float*         lse;
+  void*          workspace;
+  size_t         workspace_bytes;
+  int32_t        window;
+  int32_t        n_sink;
+  const float*   part_out;
+  const float*   part_lse;
+} tdk_prompt_attend_io;
+
+/* Depends on n_seqs, n_q, n_k and max_len only; 0 where none is needed or on bad arguments. */
+size_t     tdk_prompt_attend_workspace_bytes(const tdk_kv* kv, const tdk_prompt_batch* batch, int32_t n_q_heads);
+tdk_status tdk_prompt_attend(const tdk_kv* kv, const tdk_prompt_batch* batch, const tdk_prompt_attend_io* io, void* hip_stream);
+
 /* Storage arithmetic of Sec. 6.4 (host only). */
 double tdk_dense_bytes(const tdk_model* m, int64_t span_tokens);   /* one layer of one cache      */
 double tdk_diff_bytes(const tdk_model* m, int64_t diff_pages);     /* values + idx + count/offset */

@@ -79,6 +79,15 @@ struct KvAttendDev {
   float          scale2;       // times log2(e)
 };
 
+// Attention of rows that are not in pages: KvDev has the rows (k, v, q_start; no table), the base what both kinds share.
+struct PromptAttendDev : KvAttendDev {
+  const int32_t* k_start;
+  int64_t        k_stride, v_stride;                        // bytes
+  int32_t        n_k;          // rows of k and v
+  int32_t        f32;          // out is fp32
+  int32_t        last_id;      // row blocks from this number down; -1: from 0 up
+};
+
 // How a call of the attention is cut.
 struct KvAttendPlan {
   int32_t block_rows = 16;     // query rows (token, head of the group) per workgroup
@@ -98,6 +107,7 @@ hipError_t launch_kv_read(const KvDev& kv, const KvRowsDev& rows, int fmt, bool 
 hipError_t launch_kv8_read(const KvDev& kv, const KvRowsDev& rows, bool many, hipStream_t st);
 hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, int fmt, hipStream_t st);
 hipError_t launch_kv8_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, int64_t blocks, hipStream_t st);
+hipError_t launch_prompt_attend(const KvDev& kv, const PromptAttendDev& at, const KvAttendPlan& p, hipStream_t st);
 hipError_t launch_kv_join(const KvDev& kv, const KvAttendDev& at, int64_t rows, hipStream_t st);
 
 }  // namespace tdk

@@ -126,67 +126,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   attend_steps<FOUR ? kMx4 : kBf16>(kv, at, last_id);
 }
 
-// The parts' results of a row joined: a wavefront per row, four groups of 16 lanes that take every fourth part.  Lane l holds the weights of
-// the parts l, 64 + l, ...  Two reads in a row, weights and results (80 rows of 64 parts: 7 us; one part after the other 11, a row per 16 lanes 24).
-__global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) {
-  const int lane = threadIdx.x & 63, piece = lane & 15;
-  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (idx >= rows) return;
-  const int64_t tok = idx / at.n_q_heads;
-  if (tok < start_of(kv, 0) || tok >= start_of(kv, kv.n_seqs)) return;
-  float m[4], l[4], top = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int c = 64 * k + lane;
-    m[k] = -INFINITY;
-    l[k] = 0.f;
-    if (c < at.n_chunks) {
-      const f32x2 x = *reinterpret_cast<const f32x2*>(at.part_ml + 2 * (idx * at.n_chunks + c));
-      m[k] = part_max(x[0], x[1]);
-      l[k] = x[1];
-    }
-    top = fmaxf(top, m[k]);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const f32x4* parts = reinterpret_cast<const f32x4*>(at.part_o + idx * at.n_chunks * kHeadDim) + 2 * piece;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (64 * k >= at.n_chunks) break;
-    const float f = m[k] == -INFINITY ? 0.f : share(m[k], top, at.scale2);
-    sum += f * l[k];
-    for (int c0 = 0; c0 < 64 && 64 * k + c0 < at.n_chunks; c0 += 16) {
-      // sixteen parts a time, four of them in each lane's hands: their reads are under way together (parts with no weight are not read)
-      f32x4 x[4], y[4];
-      float w[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int c = c0 + 4 * u + (lane >> 4);
-        w[u] = __shfl(f, c);
-        x[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (w[u] == 0.f) continue;
-        x[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)];
-        y[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          o[e] += w[u] * x[u][e];
-          o[4 + e] += w[u] * y[u][e];
-        }
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    o[e] += __shfl_xor(o[e], 16);
-    o[e] += __shfl_xor(o[e], 32);
-  }
-  if (lane < 16) finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
-}
+__global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) { join_parts(kv, at, rows); }
 
 // (many tokens pass the caches by: 12 500 tokens 79 -> 74 us, 19 000 in 4 bits and back 132 -> 118.  Few stay there, also where a wavefront has all of a
 // token: 250 tokens of four heads without queries, attention to 300 tokens each behind it, 38.5 -> 38.2 us together; of 1500

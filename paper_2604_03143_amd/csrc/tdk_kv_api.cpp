@@ -28,6 +28,7 @@ constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1; // of one launch
 constexpr int32_t kMaxQHeads = 1 << 16;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;        // of a call, and of a sequence that a table has room for
 constexpr float   kMaxScale = 0x1p127f;                  // times log2(e) still an fp32 number
+constexpr int64_t kMaxKeyStride = (int64_t)1 << 24;     // elements: places in a step's tile of rows are 32-bit numbers of bytes
 constexpr int32_t kMaxSeqs = 1 << 30;                   // the search for a token's sequence counts in int32, in steps of 64
 
 bool off(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -209,9 +210,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   one part 275, six 237), and not where there are many (250 of 4000: one part 512, two 529).
 //   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
 //   many (four prompts of up to 2048 tokens: one part 523 us, two 662).
-int64_t attend_parts(const tdk_kv* kv, int64_t blocks, int64_t len, int64_t per_seq, int block_rows) {
-  const bool four = kv->fmt == kMx4;
-  const int64_t resident = (four && block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus;
+int64_t attend_parts(int64_t resident, bool four, int64_t blocks, int64_t len, int64_t per_seq) {
   const int64_t most = std::min<int64_t>((len + 255) / 256, 256);
   if (per_seq > 128 || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
   const double extra = four ? 360 + 8.0 * per_seq : 120 + 2.0 * per_seq;
@@ -253,6 +252,73 @@ tdk_status kv_create(const tdk_model* model, const tdk_rope* rope, int32_t forma
   return TDK_OK;
 }
 
+void plan_space(KvAttendPlan& p) {
+  if (p.n_chunks <= 1) return;
+  p.o_part_ml = up256((size_t)p.rows * p.n_chunks * kHeadDim * sizeof(float));
+  p.bytes = p.o_part_ml + up256((size_t)p.rows * p.n_chunks * 2 * sizeof(float));
+}
+
+// what both kinds of attention take besides their rows
+struct Shared {
+  const void* q;
+  int64_t q_stride;
+  int32_t n_q_heads;
+  float scale;
+  const void* out;
+  int64_t out_stride;
+  const float* lse;
+  const void* workspace;
+  size_t workspace_bytes;
+  int32_t window, n_sink;
+  const float *part_out, *part_lse;
+};
+
+tdk_status check_attend(const Shared& a, bool planned) {
+  if (!std::isfinite(a.scale)) return fail(TDK_ERR_INVALID_ARG, "scale must be finite");
+  if (std::fabs(a.scale) > kMaxScale) return fail(TDK_ERR_INVALID_ARG, "scale: a magnitude above 2^127");
+  if (a.window < 0 || a.n_sink < 0) return fail(TDK_ERR_INVALID_ARG, "window / n_sink is negative");
+  if (!planned) return fail(TDK_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of the KV heads");
+  if (!a.part_out != !a.part_lse) return fail(TDK_ERR_INVALID_ARG, "part_out and part_lse come together");
+  return TDK_OK;
+}
+tdk_status check_attend_buffers(const Shared& a, const KvAttendPlan& p, int32_t heads) {
+  if (!a.q || !a.out) return fail(TDK_ERR_INVALID_ARG, "attend io holds a NULL buffer");
+  if (off(a.q, 16) || off(a.out, 16)) return fail(TDK_ERR_INVALID_ARG, "q / out must be 16-byte aligned");
+  const int64_t qd = (int64_t)a.n_q_heads * kHeadDim;
+  if (bad_stride(a.q_stride, qd) || bad_stride(a.out_stride, qd))
+    return fail(TDK_ERR_INVALID_ARG, "attend io: strides must be multiples of 8, at least n_q_heads * 128");
+  if (p.bytes && !a.workspace) return fail(TDK_ERR_INVALID_ARG, "workspace is NULL");
+  if (p.bytes && off(a.workspace, 256)) return fail(TDK_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
+  if (a.workspace_bytes < p.bytes) return fail(TDK_ERR_INVALID_ARG, "workspace smaller than the call's workspace_bytes()");
+  if ((p.ids * p.n_chunks + 8) * heads * 256 > kMaxThreads || p.rows > kMaxRows)
+    return fail(TDK_ERR_UNSUPPORTED, "attention launch larger than a grid");
+  return TDK_OK;
+}
+void attend_dev(const tdk_kv* kv, const Shared& a, const KvAttendPlan& p, KvAttendDev& at) {
+  at.q = static_cast<const char*>(a.q);
+  at.out = static_cast<char*>(const_cast<void*>(a.out));
+  at.lse = const_cast<float*>(a.lse);
+  at.part_o = static_cast<float*>(const_cast<void*>(a.workspace));
+  at.part_ml = reinterpret_cast<float*>(static_cast<char*>(const_cast<void*>(a.workspace)) + p.o_part_ml);
+  at.hole = nullptr;
+  at.other_out = a.part_out;
+  at.other_lse = a.part_lse;
+  at.q_stride = 2 * a.q_stride;
+  at.out_stride = 2 * a.out_stride;
+  at.n_q_heads = a.n_q_heads;
+  at.group = a.n_q_heads / kv->model.num_kv_heads;
+  at.window = a.window;
+  at.n_sink = a.n_sink;
+  at.n_chunks = p.n_chunks;
+  at.piece_tiles = p.piece_tiles;
+  at.n_rest = (int32_t)(p.ids * p.n_chunks);
+  at.q_flip = std::signbit(a.scale) ? 1 : 0;
+  // (Zero, uniform weights, becomes the least number above it: what a row does not see stays minus infinity, and the scaled differences of all
+  // other scores are below 2^-20.)
+  at.scale = std::fmax(std::fabs(a.scale), std::numeric_limits<float>::denorm_min());
+  at.scale2 = at.scale * 1.4426950408889634f;
+}
+
 // window, n_sink: as in the call; without a window the plan is the one with the most parts.  false: bad arguments
 bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
   const int32_t H = kv->model.num_kv_heads;
@@ -276,13 +342,32 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_tokens)) : b->max_len;
   const int64_t len = std::max<int64_t>(1, seen);
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
-  p.n_chunks = (int32_t)attend_parts(kv, blocks, len, per_seq, p.block_rows);
+  const bool four = kv->fmt == kMx4;
+  p.n_chunks = (int32_t)attend_parts((four && p.block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus, four, blocks, len, per_seq);
   const int64_t tile = p.block_rows == 128 ? 64 : 32;
   p.piece_tiles = (int32_t)(((len + tile - 1) / tile + p.n_chunks - 1) / p.n_chunks);
-  if (p.n_chunks > 1) {
-    p.o_part_ml = up256((size_t)p.rows * p.n_chunks * kHeadDim * sizeof(float));
-    p.bytes = p.o_part_ml + up256((size_t)p.rows * p.n_chunks * 2 * sizeof(float));
-  }
+  plan_space(p);
+  return true;
+}
+
+// The same for rows that are not in pages.
+bool prompt_plan(const tdk_kv* kv, const tdk_prompt_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
+  const int32_t H = kv->model.num_kv_heads;
+  if (b->n_seqs < 0 || b->n_q < 0 || b->n_k < 0 || b->max_len < 0 || n_q_heads < 1 || n_q_heads % H || n_q_heads > kMaxQHeads) return false;
+  p = KvAttendPlan{};
+  p.rows = (int64_t)b->n_q * n_q_heads;
+  if (b->n_seqs == 0 || b->n_q == 0) return true;
+  const int64_t group = n_q_heads / H;
+  const int64_t per_seq = ((int64_t)b->n_q * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
+  const auto blocks_of = [&](int rows) { return (per_seq + rows - 1) / rows * b->n_seqs * H; };
+  p.block_rows = blocks_of(256) >= kv->n_cus ? 256 : 128;
+  p.forward = per_seq <= p.block_rows;
+  p.ids = (int64_t)b->n_q * group / p.block_rows + b->n_seqs;
+  const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_q)) : b->max_len;
+  const int64_t len = std::max<int64_t>(1, seen);
+  p.n_chunks = (int32_t)attend_parts((p.block_rows == 256 ? 1 : 2) * (int64_t)kv->n_cus, false, blocks_of(p.block_rows), len, per_seq);
+  p.piece_tiles = (int32_t)(((len + 63) / 64 + p.n_chunks - 1) / p.n_chunks);
+  plan_space(p);
   return true;
 }
 
@@ -332,53 +417,73 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     if (st != TDK_OK) return st;
     if (!a) return fail(TDK_ERR_INVALID_ARG, "attend io is NULL");
     KvAttendPlan p;
-    if (!std::isfinite(a->scale)) return fail(TDK_ERR_INVALID_ARG, "scale must be finite");
-    if (std::fabs(a->scale) > kMaxScale) return fail(TDK_ERR_INVALID_ARG, "scale: a magnitude above 2^127");
-    if (a->window < 0 || a->n_sink < 0) return fail(TDK_ERR_INVALID_ARG, "window / n_sink is negative");
-    if (!attend_plan_kv(kv, batch, a->n_q_heads, a->window, a->n_sink, p))
-      return fail(TDK_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of the KV heads");
-    if (!a->part_out != !a->part_lse) return fail(TDK_ERR_INVALID_ARG, "part_out and part_lse come together");
+    const Shared sh{a->q, a->q_stride, a->n_q_heads, a->scale, a->out, a->out_stride, a->lse, a->workspace, a->workspace_bytes,
+                    a->window, a->n_sink, a->part_out, a->part_lse};
+    st = check_attend(sh, attend_plan_kv(kv, batch, a->n_q_heads, std::max(a->window, 0), std::max(a->n_sink, 0), p));
+    if (st != TDK_OK) return st;
     if (off(a->part_out, 16) || off(a->part_lse, 4) || off(a->hole, 4) || off(a->lse, 4))
       return fail(TDK_ERR_INVALID_ARG, "attend io: part_out must be 16-byte aligned, part_lse, hole and lse 4-byte");
-    if (!nothing) {
-      if (!a->q || !a->out) return fail(TDK_ERR_INVALID_ARG, "attend io holds a NULL buffer");
-      if (off(a->q, 16) || off(a->out, 16)) return fail(TDK_ERR_INVALID_ARG, "q / out must be 16-byte aligned");
-      const int64_t qd = (int64_t)a->n_q_heads * kHeadDim;
-      if (bad_stride(a->q_stride, qd) || bad_stride(a->out_stride, qd))
-        return fail(TDK_ERR_INVALID_ARG, "attend io: strides must be multiples of 8, at least n_q_heads * 128");
-      if (p.bytes && !a->workspace) return fail(TDK_ERR_INVALID_ARG, "workspace is NULL");
-      if (p.bytes && off(a->workspace, 256)) return fail(TDK_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
-      if (a->workspace_bytes < p.bytes) return fail(TDK_ERR_INVALID_ARG, "workspace smaller than tdk_kv_attend_workspace_bytes()");
-      if ((p.ids * p.n_chunks + 8) * kv->model.num_kv_heads * 256 > kMaxThreads || p.rows > kMaxRows)
-        return fail(TDK_ERR_UNSUPPORTED, "attention launch larger than a grid");
-    }
+    if (!nothing && (st = check_attend_buffers(sh, p, kv->model.num_kv_heads)) != TDK_OK) return st;
     st = check_device(kv);
     if (st != TDK_OK || nothing) return st;
     KvAttendDev at;
-    at.q = static_cast<const char*>(a->q);
-    at.out = static_cast<char*>(a->out);
-    at.lse = a->lse;
-    at.part_o = static_cast<float*>(a->workspace);
-    at.part_ml = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + p.o_part_ml);
+    attend_dev(kv, sh, p, at);
     at.hole = a->hole;
-    at.other_out = a->part_out;
-    at.other_lse = a->part_lse;
-    at.q_stride = 2 * a->q_stride;
-    at.out_stride = 2 * a->out_stride;
-    at.n_q_heads = a->n_q_heads;
-    at.group = a->n_q_heads / kv->model.num_kv_heads;
-    at.window = a->window;
-    at.n_sink = a->n_sink;
-    at.n_chunks = p.n_chunks;
-    at.piece_tiles = p.piece_tiles;
-    at.n_rest = (int32_t)(p.ids * p.n_chunks);
-    at.q_flip = std::signbit(a->scale) ? 1 : 0;
-    // (Zero, uniform weights, becomes the least number above it: what a row does not see stays minus infinity, and the scaled differences of all
-    // other scores are below 2^-20.)
-    at.scale = std::fmax(std::fabs(a->scale), std::numeric_limits<float>::denorm_min());
-    at.scale2 = at.scale * 1.4426950408889634f;
     const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->fmt, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_attend)");
+  });
+}
+
+size_t tdk_prompt_attend_workspace_bytes(const tdk_kv* kv, const tdk_prompt_batch* batch, int32_t n_q_heads) {
+  KvAttendPlan p;
+  return kv && batch && prompt_plan(kv, batch, n_q_heads, 0, 0, p) ? p.bytes : 0;
+}
+
+tdk_status tdk_prompt_attend(const tdk_kv* kv, const tdk_prompt_batch* b, const tdk_prompt_attend_io* a, void* hip_stream) {
+  return guarded([&]() -> tdk_status {
+    if (!kv) return fail(TDK_ERR_INVALID_ARG, "kv handle is NULL");
+    if (!b || !a) return fail(TDK_ERR_INVALID_ARG, "batch / attend io is NULL");
+    if (b->n_seqs < 0 || b->n_q < 0 || b->n_k < 0 || b->max_len < 0) return fail(TDK_ERR_INVALID_ARG, "batch: negative size");
+    if (b->n_q > kMaxTokens || b->n_k > kMaxTokens) return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 tokens");
+    if (b->n_seqs > kMaxSeqs) return fail(TDK_ERR_UNSUPPORTED, "batch: more than 2^30 sequences");
+    const bool nothing = b->n_seqs == 0 || b->n_q == 0;
+    if (!nothing && (!b->q_start || !b->k_start)) return fail(TDK_ERR_INVALID_ARG, "batch: q_start / k_start is NULL");
+    if (off(b->q_start, 4) || off(b->k_start, 4)) return fail(TDK_ERR_INVALID_ARG, "batch: arrays must be 4-byte aligned");
+    KvAttendPlan p;
+    const Shared sh{a->q, a->q_stride, a->n_q_heads, a->scale, a->out, a->out_stride, a->lse, a->workspace, a->workspace_bytes,
+                    a->window, a->n_sink, a->part_out, a->part_lse};
+    tdk_status st = check_attend(sh, prompt_plan(kv, b, a->n_q_heads, std::max(a->window, 0), std::max(a->n_sink, 0), p));
+    if (st != TDK_OK) return st;
+    if (off(a->part_out, 16) || off(a->part_lse, 4) || off(a->lse, 4))
+      return fail(TDK_ERR_INVALID_ARG, "attend io: part_out must be 16-byte aligned, part_lse and lse 4-byte");
+    if (!nothing) {
+      if ((st = check_attend_buffers(sh, p, kv->model.num_kv_heads)) != TDK_OK) return st;
+      const int64_t hd = (int64_t)kv->model.num_kv_heads * kHeadDim;
+      if (b->n_k > 0 && (!a->k || !a->v)) return fail(TDK_ERR_INVALID_ARG, "attend io: k / v is NULL");
+      if (off(a->k, 16) || off(a->v, 16)) return fail(TDK_ERR_INVALID_ARG, "k / v must be 16-byte aligned");
+      if (bad_stride(a->k_stride, hd) || bad_stride(a->v_stride, hd) || a->k_stride > kMaxKeyStride || a->v_stride > kMaxKeyStride)
+        return fail(TDK_ERR_INVALID_ARG, "attend io: k and v strides must be multiples of 8, at least num_kv_heads * 128 and at most 2^24");
+    }
+    st = check_device(kv);
+    if (st != TDK_OK || nothing) return st;
+    KvDev d{};
+    d.k = static_cast<char*>(const_cast<void*>(a->k));
+    d.v = static_cast<char*>(const_cast<void*>(a->v));
+    d.q_start = b->q_start;
+    d.n_seqs = b->n_seqs;
+    d.n_tokens = b->n_q;
+    d.heads = kv->model.num_kv_heads;
+    PromptAttendDev at;
+    attend_dev(kv, sh, p, at);
+    at.k_start = b->k_start;
+    at.k_stride = 2 * a->k_stride;
+    at.v_stride = 2 * a->v_stride;
+    at.n_k = b->n_k;
+    at.f32 = a->out_f32 != 0;
+    if (at.f32) at.out_stride *= 2;
+    at.last_id = p.forward ? -1 : (int32_t)(p.ids - 1);
+    const hipError_t e = launch_prompt_attend(d, at, p, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_prompt_attend)");
   });
 }
 

@@ -311,7 +311,8 @@ __device__ __forceinline__ float moved(float m, float mx, float scale2) { return
 __device__ __forceinline__ float share(float m, float ref, float scale2) { return __builtin_amdgcn_exp2f((m - ref) * scale2); }
 
 // Eight elements of a finished row (un-normalised sums o, reference point m, sum l): joined with the caller's partial result and written.
-__device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int hq, int piece, const float (&o)[8], float m, float l) {
+template <class At>
+__device__ __forceinline__ void finish(const At& at, int64_t tok, int hq, int piece, const float (&o)[8], float m, float l) {
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
   float r[8];
 #pragma unroll
@@ -330,6 +331,15 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
       lse = top + __logf(both);
     }
   }
+  if constexpr (!std::is_same_v<At, KvAttendDev>) {
+    if (at.f32) {
+      if (at.lse && piece == 0) at.lse[idx] = lse;
+      f32x4* dst = reinterpret_cast<f32x4*>(at.out + tok * at.out_stride + hq * (2 * kRow) + 32 * piece);
+      dst[0] = f32x4{r[0], r[1], r[2], r[3]};
+      dst[1] = f32x4{r[4], r[5], r[6], r[7]};
+      return;
+    }
+  }
   u32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = pack2(r[2 * i], r[2 * i + 1]);
@@ -338,7 +348,8 @@ __device__ __forceinline__ void finish(const KvAttendDev& at, int64_t tok, int h
 }
 
 // The same for a workgroup's part: finished if it is the only one, else kept for the join.
-__device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m, float l) {
+template <class At>
+__device__ __forceinline__ void put_row(const At& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m, float l) {
   if (at.n_chunks == 1) {
     finish(at, tok, hq, piece, o, m, l);
     return;
@@ -1133,6 +1144,69 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
   }
 }
 
+
+// The parts' results of a row joined: a wavefront per row, four groups of 16 lanes that take every fourth part.  Lane l holds the weights of
+// the parts l, 64 + l, ...  Two reads in a row, weights and results (80 rows of 64 parts: 7 us; one part after the other 11, a row per 16 lanes 24).
+template <class At>
+__device__ __forceinline__ void join_parts(const KvDev kv, const At at, int64_t rows) {
+  const int lane = threadIdx.x & 63, piece = lane & 15;
+  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (idx >= rows) return;
+  const int64_t tok = idx / at.n_q_heads;
+  if (tok < start_of(kv, 0) || tok >= start_of(kv, kv.n_seqs)) return;
+  float m[4], l[4], top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int c = 64 * k + lane;
+    m[k] = -INFINITY;
+    l[k] = 0.f;
+    if (c < at.n_chunks) {
+      const f32x2 x = *reinterpret_cast<const f32x2*>(at.part_ml + 2 * (idx * at.n_chunks + c));
+      m[k] = part_max(x[0], x[1]);
+      l[k] = x[1];
+    }
+    top = fmaxf(top, m[k]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  float sum = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const f32x4* parts = reinterpret_cast<const f32x4*>(at.part_o + idx * at.n_chunks * kHeadDim) + 2 * piece;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (64 * k >= at.n_chunks) break;
+    const float f = m[k] == -INFINITY ? 0.f : share(m[k], top, at.scale2);
+    sum += f * l[k];
+    for (int c0 = 0; c0 < 64 && 64 * k + c0 < at.n_chunks; c0 += 16) {
+      // sixteen parts a time, four of them in each lane's hands: their reads are under way together (parts with no weight are not read)
+      f32x4 x[4], y[4];
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = c0 + 4 * u + (lane >> 4);
+        w[u] = __shfl(f, c);
+        x[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (w[u] == 0.f) continue;
+        x[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)];
+        y[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[e] += w[u] * x[u][e];
+          o[4 + e] += w[u] * y[u][e];
+        }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    o[e] += __shfl_xor(o[e], 16);
+    o[e] += __shfl_xor(o[e], 32);
+  }
+  if (lane < 16) finish(at, tok, (int)(idx - tok * at.n_q_heads), piece, o, top, sum);
+}
 
 template <class... A>
 hipError_t launch(void (*kernel)(A...), int64_t blocks, int threads, hipStream_t st, std::common_type_t<A>... args) {

@@ -39,7 +39,7 @@ EXPORTS = (
     "tdk_prompt_plan_create", "tdk_prompt_plan_destroy", "tdk_prompt_plan_n_sessions", "tdk_prompt_plan_span",
     "tdk_prompt_plan_session_of", "tdk_prompt_plan_segments",
     "tdk_kv_create", "tdk_kv_create_rope", "tdk_kv_destroy", "tdk_kv_page_bytes", "tdk_kv_append", "tdk_kv_read", "tdk_kv_rotate",
-    "tdk_kv_attend_workspace_bytes", "tdk_kv_attend",
+    "tdk_kv_attend_workspace_bytes", "tdk_kv_attend", "tdk_prompt_attend_workspace_bytes", "tdk_prompt_attend",
     "tdk_timing_enable", "tdk_timing_read", "tdk_timing_reset",
     "tdk_dense_bytes", "tdk_diff_bytes", "tdk_family_cost",
     "tdk_util_copy", "tdk_util_fill", "tdk_util_page_fill", "tdk_util_page_read",
@@ -126,6 +126,18 @@ class KvAttendIO(C.Structure):
                 ("part_lse", C.c_void_p)]
 
 
+class PromptBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_q", C.c_int32), ("n_k", C.c_int32), ("max_len", C.c_int32), ("q_start", C.c_void_p),
+                ("k_start", C.c_void_p)]
+
+
+class PromptAttendIO(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("n_q_heads", C.c_int32), ("k", C.c_void_p), ("k_stride", C.c_int64),
+                ("v", C.c_void_p), ("v_stride", C.c_int64), ("scale", C.c_float), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("out_f32", C.c_int32), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("window", C.c_int32), ("n_sink", C.c_int32), ("part_out", C.c_void_p), ("part_lse", C.c_void_p)]
+
+
 class TdkError(RuntimeError):
     def __init__(self, status: int, what: str, detail: str):
         super().__init__(f"{what}: status {status} ({detail})")
@@ -193,6 +205,9 @@ def load() -> C.CDLL:
     L.tdk_kv_attend_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(KvBatch), C.c_int32]
     L.tdk_kv_attend_workspace_bytes.restype = C.c_size_t
     L.tdk_kv_attend.argtypes = [C.c_void_p, C.POINTER(KvCache), C.POINTER(KvBatch), C.POINTER(KvAttendIO), C.c_void_p]
+    L.tdk_prompt_attend_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(PromptBatch), C.c_int32]
+    L.tdk_prompt_attend_workspace_bytes.restype = C.c_size_t
+    L.tdk_prompt_attend.argtypes = [C.c_void_p, C.POINTER(PromptBatch), C.POINTER(PromptAttendIO), C.c_void_p]
     L.tdk_timing_enable.argtypes = [C.c_void_p, C.c_int32]
     L.tdk_timing_read.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     L.tdk_timing_reset.argtypes = [C.c_void_p]
@@ -533,6 +548,25 @@ def tdk_kv_attend_workspace_bytes(kv: Kv, batch: KvBatch, n_q_heads: int) -> int
 
 def tdk_kv_attend(kv: Kv, cache: KvCache, batch: KvBatch, a: KvAttendIO, stream: int = 0) -> None:
     _check(load().tdk_kv_attend(kv.handle, C.byref(cache), C.byref(batch), C.byref(a), C.c_void_p(stream)), "tdk_kv_attend")
+
+
+def prompt_batch(n_seqs: int, n_q: int, n_k: int, max_len: int, q_start, k_start) -> PromptBatch:
+    return PromptBatch(int(n_seqs), int(n_q), int(n_k), int(max_len), _ptr(q_start), _ptr(k_start))
+
+
+def prompt_attend_io(q, q_stride: int, n_q_heads: int, k, k_stride: int, v, v_stride: int, scale: float, out, out_stride: int, lse, workspace,
+                     workspace_bytes: int, window: int = 0, n_sink: int = 0, part_out=None, part_lse=None, out_f32: bool = False) -> PromptAttendIO:
+    return PromptAttendIO(_ptr(q), int(q_stride), int(n_q_heads), _ptr(k), int(k_stride), _ptr(v), int(v_stride), float(scale), _ptr(out),
+                          int(out_stride), int(bool(out_f32)), _ptr(lse), _ptr(workspace), int(workspace_bytes), int(window), int(n_sink),
+                          _ptr(part_out), _ptr(part_lse))
+
+
+def tdk_prompt_attend_workspace_bytes(kv: Kv, batch: PromptBatch, n_q_heads: int) -> int:
+    return int(load().tdk_prompt_attend_workspace_bytes(kv.handle, C.byref(batch), int(n_q_heads)))
+
+
+def tdk_prompt_attend(kv: Kv, batch: PromptBatch, io: PromptAttendIO, stream: int = 0) -> None:
+    _check(load().tdk_prompt_attend(kv.handle, C.byref(batch), C.byref(io), C.c_void_p(stream)), "tdk_prompt_attend")
 
 
 def tdk_timing_enable(r: Round, on: bool) -> None:
