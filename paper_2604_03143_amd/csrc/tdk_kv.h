@@ -85,7 +85,9 @@ struct PromptAttendDev : KvAttendDev {
   int64_t        k_stride, v_stride;                        // bytes
   int32_t        n_k;          // rows of k and v
   int32_t        f32;          // out is fp32
-  int32_t        last_id;      // row blocks from this number down; -1: from 0 up
+  int32_t        down;         // row blocks: so many from last_id down, the others from 0 up
+  int32_t        last_id;
+  uint32_t       group_inv;    // 2^22 / group, rounded up
 };
 
 // How a call of the attention is cut.

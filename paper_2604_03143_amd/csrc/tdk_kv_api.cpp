@@ -350,6 +350,21 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   return true;
 }
 
+// Parts of a prompt's keys: what a call takes in us with each number of them.  A workgroup's step takes 1.1 alone on its compute unit, 2 beside
+// another; its start and end 6; the parts' results go to memory and back at 4 TB/s, in a launch of their own.
+int64_t prompt_parts(int64_t n_cus, int64_t blocks, int64_t steps, int64_t rows) {
+  const int64_t most = std::min<int64_t>((steps + 3) / 4, 256);
+  int64_t best = 1;
+  double least = INFINITY;
+  for (int64_t c = 1; c <= most; ++c) {
+    const int64_t groups = blocks * c, rounds = (groups + 2 * n_cus - 1) / (2 * n_cus);
+    const double cost = rounds * ((groups <= n_cus ? 1.1 : 2.0) * ((steps + c - 1) / c) + 6.0) + (c > 1 ? 5.0 + rows * c * 1040.0 / 4e6 : 0.0);
+    if (cost < least) { least = cost; best = c; }
+    if (rounds > 2) break;
+  }
+  return best;
+}
+
 // The same for rows that are not in pages.
 bool prompt_plan(const tdk_kv* kv, const tdk_prompt_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
   const int32_t H = kv->model.num_kv_heads;
@@ -359,14 +374,15 @@ bool prompt_plan(const tdk_kv* kv, const tdk_prompt_batch* b, int32_t n_q_heads,
   if (b->n_seqs == 0 || b->n_q == 0) return true;
   const int64_t group = n_q_heads / H;
   const int64_t per_seq = ((int64_t)b->n_q * group + b->n_seqs - 1) / b->n_seqs;      // rows of a sequence and KV head, on average
-  const auto blocks_of = [&](int rows) { return (per_seq + rows - 1) / rows * b->n_seqs * H; };
-  p.block_rows = blocks_of(256) >= kv->n_cus ? 256 : 128;
+  p.block_rows = 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_q * group / p.block_rows + b->n_seqs;
   const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_q)) : b->max_len;
-  const int64_t len = std::max<int64_t>(1, seen);
-  p.n_chunks = (int32_t)attend_parts((p.block_rows == 256 ? 1 : 2) * (int64_t)kv->n_cus, false, blocks_of(p.block_rows), len, per_seq);
-  p.piece_tiles = (int32_t)(((len + 63) / 64 + p.n_chunks - 1) / p.n_chunks);
+  const auto steps_of = [](int64_t len) { return std::max<int64_t>(1, (len + 63) / 64); };
+  const int64_t steps = steps_of(seen), blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
+  p.n_chunks = (int32_t)prompt_parts(kv->n_cus, blocks, steps_of(b->max_len), p.rows);      // (the workspace has room for so many, whatever the window)
+  if (seen < b->max_len) p.n_chunks = std::min(p.n_chunks, (int32_t)prompt_parts(kv->n_cus, blocks, steps, p.rows));
+  p.piece_tiles = (int32_t)((steps + p.n_chunks - 1) / p.n_chunks);
   plan_space(p);
   return true;
 }
@@ -481,7 +497,14 @@ tdk_status tdk_prompt_attend(const tdk_kv* kv, const tdk_prompt_batch* b, const 
     at.n_k = b->n_k;
     at.f32 = a->out_f32 != 0;
     if (at.f32) at.out_stride *= 2;
-    at.last_id = p.forward ? -1 : (int32_t)(p.ids - 1);
+    // Blocks of one length of rows (a block per sequence) as they come; else a causal prompt's last rows see most and start first.  One sequence whose
+    // blocks all find room at once, two on a compute unit: the second half the other way round, so that long ones have short ones beside them (8192 tokens
+    // and 8 heads with a query each: 181 -> 172 us).
+    at.last_id = (int32_t)(p.ids - 1);
+    at.down = p.forward ? 0 : (int32_t)p.ids;
+    const int64_t full = (p.rows / d.heads + 127) / 128, room = kv->n_cus / d.heads;      // blocks of one sequence and KV head, compute units for them
+    if (!p.forward && b->n_seqs == 1 && p.n_chunks == 1 && full <= 2 * room) at.down = (int32_t)std::min<int64_t>(p.ids, room + p.ids - full);
+    at.group_inv = (uint32_t)(((1u << 22) + at.group - 1) / at.group);
     const hipError_t e = launch_prompt_attend(d, at, p, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_prompt_attend)");
   });
