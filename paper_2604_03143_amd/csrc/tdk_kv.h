@@ -77,6 +77,8 @@ struct KvAttendDev {
   int32_t        q_flip;       // the caller's scale was negative: the queries carry the sign
   float          scale;        // its magnitude, not zero
   float          scale2;       // times log2(e)
+  uint32_t       group_inv;    // 2^22 / group, rounded up
+  int32_t        last_id;      // row blocks from this number down; -1: from 0 up
 };
 
 // Attention of rows that are not in pages: KvDev has the rows (k, v, q_start; no table), the base what both kinds share.
@@ -86,8 +88,6 @@ struct PromptAttendDev : KvAttendDev {
   int32_t        n_k;          // rows of k and v
   int32_t        f32;          // out is fp32
   int32_t        down;         // row blocks: so many from last_id down, the others from 0 up
-  int32_t        last_id;
-  uint32_t       group_inv;    // 2^22 / group, rounded up
 };
 
 // How a call of the attention is cut.

@@ -1,7 +1,128 @@
-// The kernels of the paged caches in 8 bits (tdk_kv_pages.h has their bodies; tdk_rope.hip the append).
-#include "tdk_kv_pages.h"
+// The kernels of the paged caches in 8 bits (tdk_rope.hip has the append).
+#include "tdk_steps.h"
 
 namespace tdk {
+
+namespace {
+
+// Pages in 8 bits by way of registers, where they become bf16.  Lane l of wavefront w brings 16 bytes (l % 8) of the tokens 16 w + 8 i + l / 8 of
+// a step: what is written to LDS at a step's start was asked for at the start of the one before.
+struct Codes8 {
+  u32x4 c[2];
+  uint32_t e[2];                             // their exponents
+};
+
+struct PageSource {
+  using At = KvAttendDev;
+  static constexpr bool kHoles = true, kSpread = false;
+  static __device__ __forceinline__ bool wide(const At&) { return false; }
+
+  Tiles tiles;
+  int total;
+  __device__ __forceinline__ bool find(const KvDev& kv, const At& at, int place, int lane, Block& b) {
+    if (!find_block(kv, at, at.last_id < 0 ? place : at.last_id - place, kRows, lane, b)) return false;
+    tiles = tiles_of(kv, at, b, kStep);
+    total = tiles.total;
+    return true;
+  }
+
+  const KvDev* cache;
+  const At* a;
+  const Block* blk;
+  StepTiles* sh;
+  PageList<4> pages;
+  Codes8 ck, cv;
+  int h, t_begin, t_end, wave, lane;
+  __device__ __forceinline__ Codes8 fetch(const char* plane, const Pages<4>& pg) const {
+    const int T = 1 << cache->page_shift;
+    const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
+    const int row0 = 16 * wave & (T - 1);
+    const char* base = plane + (page * cache->heads + h) * (T * (kRow8 + 4));
+    Codes8 x;
+    x.c[0] = *reinterpret_cast<const u32x4*>(base + row0 * kRow8 + 16 * lane);
+    x.c[1] = *reinterpret_cast<const u32x4*>(base + row0 * kRow8 + 1024 + 16 * lane);
+    const char* e = base + (T * kRow8 + row0 * 4) + (lane >> 1);
+    x.e[0] = *reinterpret_cast<const uint8_t*>(e);
+    x.e[1] = *reinterpret_cast<const uint8_t*>(e + 32);
+    return x;
+  }
+  template <bool V>
+  __device__ __forceinline__ void put(const Codes8& x, unsigned char* tile) const {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));             // (the places in the tiles are worked out again: kept from step to step they spill)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = 16 * wave + 8 * i + (ln >> 3);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = 2 * (ln & 7) + e;
+        *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from8(x.c[i][2 * e], x.c[i][2 * e + 1], x.e[i]);
+      }
+    }
+  }
+  // V of a step that some rows see and some do not, before it is put there: what none sees becomes zero (a weight of zero would not silence infinity
+  // or NaN), and the tile's flag says whether what is left is finite.
+  __device__ __forceinline__ void check(int i, int there, int place, Codes8& x) const {
+    const int j0 = tiles.tile(i) * kStep;
+    bool mine = false;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (!((there >> wave & 1) && one_sees(*a, *blk, j0 + 16 * wave + 8 * k + (lane >> 3)))) {
+        x.c[k] = u32x4{0, 0, 0, 0};
+        x.e[k] = 0;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 v = from8(x.c[k][2 * e], x.c[k][2 * e + 1], x.e[k]);
+        mine |= odd16(v[0]) || odd16(v[1]) || odd16(v[2]) || odd16(v[3]);
+      }
+    }
+    const int any = __any(mine);
+    if (lane == 0) sh->odd[place][wave] = any;
+  }
+  __device__ __forceinline__ void open(const KvDev& kv, const At& at, const Block& b, int head, int begin, int end, StepTiles& to, int lane_, int wave_) {
+    cache = &kv;
+    a = &at;
+    blk = &b;
+    sh = &to;
+    h = head;
+    t_begin = begin;
+    t_end = end;
+    lane = lane_;
+    wave = wave_;
+    // (Behind the last step the last one's pages are read again: what that gives is not used.)
+    if (begin < end) pages.start(kv, b.s, tiles, begin, 1, end, lane);
+  }
+  __device__ __forceinline__ int token(int i) const { return tiles.tile(i) * kStep; }
+  __device__ __forceinline__ int ok(int d) const { return there(pages.get(d)); }      // of the d-th step behind the current one
+  __device__ __forceinline__ bool seen(int i, int there) const {
+    const int j0 = token(i);
+    return there == 15 && all_see(*a, *blk, j0, j0 + kStep - 1);
+  }
+  __device__ __forceinline__ bool whole(int i) const { return seen(i, ok(i == t_begin ? 0 : 1)); }
+  __device__ __forceinline__ void first() {
+    const Codes8 k0 = fetch(cache->k, pages.get(0)), k1 = fetch(cache->k, pages.get(1));
+    Codes8 v0 = fetch(cache->v, pages.get(0));
+    ck = fetch(cache->k, pages.get(2));
+    cv = fetch(cache->v, pages.get(1));
+    put<false>(k0, sh->k[1]);
+    const int there0 = ok(0);
+    if (!seen(t_begin, there0)) check(t_begin, there0, 0, v0);
+    put<true>(v0, sh->v[0]);
+    put<false>(k1, sh->k[0]);
+  }
+  __device__ __forceinline__ void bring(int i, int place, bool to_check) {
+    put<false>(ck, sh->k[place]);
+    if (to_check) check(i + 1, ok(1), place, cv);
+    put<true>(cv, sh->v[place]);
+    ck = fetch(cache->k, pages.get(3));
+    cv = fetch(cache->v, pages.get(2));
+    pages.next(*cache, blk->s, tiles, t_begin, 1, t_end, lane);
+  }
+  __device__ __forceinline__ void arrived(int, int, bool) const {}
+};
+
+}  // namespace
 
 template <bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv8_read_kernel(const KvDev kv, const KvRowsDev rows) {
@@ -13,9 +134,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   attend_rows<kMx8, NR>(kv, at);
 }
 
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv8_attend_tile_kernel(const KvDev kv, const KvAttendDev at,
-                                                                                                             const int last_id) {
-  attend_steps<kMx8>(kv, at, last_id);
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv8_attend_tile_kernel(const KvDev kv, const KvAttendDev at) {
+  attend_in_steps<PageSource>(kv, at);
 }
 
 hipError_t launch_kv8_read(const KvDev& kv, const KvRowsDev& rows, bool many, hipStream_t st) {
@@ -23,7 +143,7 @@ hipError_t launch_kv8_read(const KvDev& kv, const KvRowsDev& rows, bool many, hi
 }
 
 hipError_t launch_kv8_attend(const KvDev& kv, const KvAttendDev& at, const KvAttendPlan& p, int64_t blocks, hipStream_t st) {
-  if (p.block_rows == 128) return launch(tdk_kv8_attend_tile_kernel, blocks, 256, st, kv, at, p.forward ? -1 : (int)(p.ids - 1));
+  if (p.block_rows == 128) return launch(tdk_kv8_attend_tile_kernel, blocks, 256, st, kv, at);
   return launch(p.block_rows == 32 ? tdk_kv8_attend_rows_kernel<2> : tdk_kv8_attend_rows_kernel<1>, blocks, 256, st, kv, at);
 }
 

@@ -307,6 +307,7 @@ void attend_dev(const tdk_kv* kv, const Shared& a, const KvAttendPlan& p, KvAtte
   at.out_stride = 2 * a.out_stride;
   at.n_q_heads = a.n_q_heads;
   at.group = a.n_q_heads / kv->model.num_kv_heads;
+  at.group_inv = (uint32_t)(((1u << 22) + at.group - 1) / at.group);
   at.window = a.window;
   at.n_sink = a.n_sink;
   at.n_chunks = p.n_chunks;
@@ -445,6 +446,7 @@ tdk_status tdk_kv_attend(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_
     KvAttendDev at;
     attend_dev(kv, sh, p, at);
     at.hole = a->hole;
+    at.last_id = p.forward ? -1 : (int32_t)(p.ids - 1);
     const hipError_t e = launch_kv_attend(kv_dev(kv, cache, batch), at, p, kv->fmt, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_kv_attend)");
   });
@@ -504,7 +506,6 @@ tdk_status tdk_prompt_attend(const tdk_kv* kv, const tdk_prompt_batch* b, const 
     at.down = p.forward ? 0 : (int32_t)p.ids;
     const int64_t full = (p.rows / d.heads + 127) / 128, room = kv->n_cus / d.heads;      // blocks of one sequence and KV head, compute units for them
     if (!p.forward && b->n_seqs == 1 && p.n_chunks == 1 && full <= 2 * room) at.down = (int32_t)std::min<int64_t>(p.ids, room + p.ids - full);
-    at.group_inv = (uint32_t)(((1u << 22) + at.group - 1) / at.group);
     const hipError_t e = launch_prompt_attend(d, at, p, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? TDK_OK : hip_fail(e, "kernel launch (tdk_prompt_attend)");
   });

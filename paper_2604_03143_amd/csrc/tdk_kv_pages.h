@@ -809,50 +809,25 @@ __device__ __forceinline__ void fetch_step(const KvDev& kv, const char* plane, c
   }
 }
 
-// 4 bits: lane l of wavefront w holds block l % 4 of token 16 w + l / 4.  8 bits: 16 bytes (l % 8) of the tokens 16 w + 8 i + l / 8.
-template <int FMT>
+// 4 bits: lane l of wavefront w holds block l % 4 of token 16 w + l / 4.
 struct Codes {
-  static constexpr int kPieces = FMT == kMx8 ? 2 : 1;
-  u32x4 c[kPieces];
-  uint32_t e[kPieces];
+  u32x4 c;
+  uint32_t e;
 };
-template <int FMT>
-__device__ __forceinline__ Codes<FMT> fetch_codes(const KvDev& kv, const char* plane, const Pages<4>& pg, int h, int wave, int lane) {
+__device__ __forceinline__ Codes fetch_codes(const KvDev& kv, const char* plane, const Pages<4>& pg, int h, int wave, int lane) {
   const int T = 1 << kv.page_shift;
   const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
   const int row0 = 16 * wave & (T - 1);
-  const char* base = plane + (page * kv.heads + h) * (T * (code_bytes(FMT) + 4));
-  if constexpr (FMT == kMx4) {
-    return Codes<FMT>{{*reinterpret_cast<const u32x4*>(base + row0 * kRow4 + 16 * lane)}, {*reinterpret_cast<const uint8_t*>(base + (T * kRow4 + row0 * 4) + lane)}};
-  } else {
-    Codes<FMT> x;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x.c[i] = *reinterpret_cast<const u32x4*>(base + row0 * kRow8 + 1024 * i + 16 * lane);
-      x.e[i] = *reinterpret_cast<const uint8_t*>(base + (T * kRow8 + row0 * 4) + 32 * i + (lane >> 1));
-    }
-    return x;
-  }
+  const char* base = plane + (page * kv.heads + h) * (T * 68);
+  return Codes{*reinterpret_cast<const u32x4*>(base + row0 * kRow4 + 16 * lane), *reinterpret_cast<const uint8_t*>(base + (T * kRow4 + row0 * 4) + lane)};
 }
-template <bool V, int FMT>
-__device__ __forceinline__ void put_codes(const Codes<FMT>& x, unsigned char* tile, int wave, int lane) {
-  if constexpr (FMT == kMx4) {
-    const int t = 16 * wave + (lane >> 2);
+template <bool V>
+__device__ __forceinline__ void put_codes(const Codes& x, unsigned char* tile, int wave, int lane) {
+  const int t = 16 * wave + (lane >> 2);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = 4 * (lane & 3) + e;
-      *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from4(x.c[0][e], x.e[0]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int t = 16 * wave + 8 * i + (lane >> 3);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = 2 * (lane & 7) + e;
-        *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from8(x.c[i][2 * e], x.c[i][2 * e + 1], x.e[i]);
-      }
-    }
+  for (int e = 0; e < 4; ++e) {
+    const int c = 4 * (lane & 3) + e;
+    *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from4(x.c[e], x.e);
   }
 }
 
@@ -999,30 +974,13 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
     }
     if (lane == 0) sh.odd[buf][wave] = any;
   };
-  // the same of 4-bit and 8-bit values, before they are put there
-  const auto check_codes = [&](int i, int ok, int buf, Codes<FMT>& x) __attribute__((always_inline)) {
+  // the same of 4-bit values, before they are put there
+  const auto check_codes = [&](int i, int ok, int buf, Codes& x) __attribute__((always_inline)) {
     const int j0 = tiles.tile(i) * kBigTile;
     int any = 0;
     if (ok != 15 || !all_see(at, b, j0, j0 + kBigTile - 1)) {
-      if constexpr (FMT == kMx4) {
-        if (!((ok >> wave & 1) && one_sees(at, b, j0 + 16 * wave + (lane >> 2)))) x = Codes<FMT>{{u32x4{0, 0, 0, 0}}, {0}};
-        any = __any(x.e[0] >= kWide4);
-      } else if constexpr (FMT == kMx8) {
-        bool mine = false;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (!((ok >> wave & 1) && one_sees(at, b, j0 + 16 * wave + 8 * k + (lane >> 3)))) {
-            x.c[k] = u32x4{0, 0, 0, 0};
-            x.e[k] = 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const u32x4 v = from8(x.c[k][2 * e], x.c[k][2 * e + 1], x.e[k]);
-            mine |= odd16(v[0]) || odd16(v[1]) || odd16(v[2]) || odd16(v[3]);
-          }
-        }
-        any = __any(mine);
-      }
+      if (!((ok >> wave & 1) && one_sees(at, b, j0 + 16 * wave + (lane >> 2)))) x = Codes{u32x4{0, 0, 0, 0}, 0};
+      any = __any(x.e >= kWide4);
     }
     if (lane == 0) sh.odd[buf][wave] = any;
   };
@@ -1033,14 +991,14 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
     PageList<4> pages;
     pages.start(kv, b.s, tiles, t_begin, 1, t_end, lane);
     int ok = there(pages.get(0));
-    Codes<FMT> ck[2], cv[2];                 // 4 and 8 bits: K of the step behind the next and V of the next one, and both of the step after
+    Codes ck[2], cv[2];                      // 4 bits: K of the step behind the next and V of the next one, and both of the step after
     if constexpr (FMT != kBf16) {
-      const Codes<FMT> k0 = fetch_codes<FMT>(kv, kv.k, pages.get(0), h, wave, lane), k1 = fetch_codes<FMT>(kv, kv.k, pages.get(1), h, wave, lane);
-      Codes<FMT> v0 = fetch_codes<FMT>(kv, kv.v, pages.get(0), h, wave, lane);
-      ck[0] = fetch_codes<FMT>(kv, kv.k, pages.get(2), h, wave, lane);
-      cv[0] = fetch_codes<FMT>(kv, kv.v, pages.get(1), h, wave, lane);
-      ck[1] = fetch_codes<FMT>(kv, kv.k, pages.get(3), h, wave, lane);
-      cv[1] = fetch_codes<FMT>(kv, kv.v, pages.get(2), h, wave, lane);
+      const Codes k0 = fetch_codes(kv, kv.k, pages.get(0), h, wave, lane), k1 = fetch_codes(kv, kv.k, pages.get(1), h, wave, lane);
+      Codes v0 = fetch_codes(kv, kv.v, pages.get(0), h, wave, lane);
+      ck[0] = fetch_codes(kv, kv.k, pages.get(2), h, wave, lane);
+      cv[0] = fetch_codes(kv, kv.v, pages.get(1), h, wave, lane);
+      ck[1] = fetch_codes(kv, kv.k, pages.get(3), h, wave, lane);
+      cv[1] = fetch_codes(kv, kv.v, pages.get(2), h, wave, lane);
       put_codes<false>(k0, sh.k[0], wave, lane);
       check_codes(t_begin, ok, 0, v0);
       put_codes<true>(v0, sh.v[0], wave, lane);
@@ -1080,8 +1038,8 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
         put_codes<false>(ck[odd], sh.k[odd], wave, ln);
         if (i + 1 < t_end) check_codes(i + 1, ok_next, odd ^ 1, cv[odd]);
         put_codes<true>(cv[odd], sh.v[odd ^ 1], wave, ln);
-        ck[odd] = fetch_codes<FMT>(kv, kv.k, pages.get(4), h, wave, lane);
-        cv[odd] = fetch_codes<FMT>(kv, kv.v, pages.get(3), h, wave, lane);
+        ck[odd] = fetch_codes(kv, kv.k, pages.get(4), h, wave, lane);
+        cv[odd] = fetch_codes(kv, kv.v, pages.get(3), h, wave, lane);
       } else {
         fetch_step(kv, kv.k, pages.get(2), h, ld, ld.k_off, lds_k[odd]);
         fetch_step(kv, kv.v, pages.get(1), h, ld, ld.v_off, lds_v[odd ^ 1]);
