@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libtdk.so")
 SOURCES = [os.path.join(CSRC, "tdk_kernels.hip"), os.path.join(CSRC, "tdk_attend.hip"), os.path.join(CSRC, "tdk_api.cpp"), os.path.join(CSRC, "tdk_plan.cpp"), os.path.join(CSRC, "tdk_prompt.cpp"),
            os.path.join(CSRC, "tdk_kv.hip"), os.path.join(CSRC, "tdk_kv8.hip"), os.path.join(CSRC, "tdk_rope.hip"), os.path.join(CSRC, "tdk_prompt_attend.hip"),
            os.path.join(CSRC, "tdk_kv_api.cpp")]
-HEADERS = [os.path.join(CSRC, "tdk_internal.h"), os.path.join(CSRC, "tdk_errors.h"), os.path.join(CSRC, "tdk_kv.h"), os.path.join(CSRC, "tdk_kv_pages.h"), os.path.join(CSRC, "tdk_tiles.h"), os.path.join(CSRC, "tdk_types.h"), os.path.join(CSRC, "tdk_plan.h"), os.path.join(ROOT, "include", "tdk.h"), os.path.join(ROOT, "include", "tdk_bench.h")]
+HEADERS = [os.path.join(CSRC, "tdk_internal.h"), os.path.join(CSRC, "tdk_errors.h"), os.path.join(CSRC, "tdk_kv.h"), os.path.join(CSRC, "tdk_kv_pages.h"), os.path.join(CSRC, "tdk_steps.h"), os.path.join(CSRC, "tdk_tiles.h"), os.path.join(CSRC, "tdk_types.h"), os.path.join(CSRC, "tdk_plan.h"), os.path.join(ROOT, "include", "tdk.h"), os.path.join(ROOT, "include", "tdk_bench.h")]
 
 
 def hipcc_command(out: str = LIB, extra=()):

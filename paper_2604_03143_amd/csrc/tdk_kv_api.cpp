@@ -208,17 +208,19 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   their way to memory and back, here in tokens.  The last round ends late on some compute units, a tenth of a round; so
 //   many parts pay where there are few rounds (64 sequences of 16 000 tokens, one round 725 us, four 680; 66 of 4000 with 20 rows,
 //   one part 275, six 237), and not where there are many (250 of 4000: one part 512, two 529).
+//   8 bits: the launch that joins the parts counts as well, as 300 tokens (100 sequences of 2000 tokens, three parts 82 us, one 68; 64 of 16 000, one part
+//   315, five 297).
 //   More (prompts): only as many as fill the device; the blocks differ in length by themselves, and a part's rows are
 //   many (four prompts of up to 2048 tokens: one part 523 us, two 662).
-int64_t attend_parts(int64_t resident, bool four, int64_t blocks, int64_t len, int64_t per_seq) {
+int64_t attend_parts(int64_t resident, int fmt, int64_t blocks, int64_t len, int64_t per_seq) {
   const int64_t most = std::min<int64_t>((len + 255) / 256, 256);
   if (per_seq > 128 || blocks >= 16 * resident) return std::max<int64_t>(1, std::min((resident + blocks - 1) / blocks, most));
-  const double extra = four ? 360 + 8.0 * per_seq : 120 + 2.0 * per_seq;
+  const double extra = fmt == kMx4 ? 360 + 8.0 * per_seq : fmt == kMx8 ? 110 + 4.0 * per_seq : 120 + 2.0 * per_seq, join = fmt == kMx8 ? 300 : 0;
   int64_t best = 1;
   double least = INFINITY;
   for (int64_t c = 1; c <= most; ++c) {
     const int64_t rounds = (blocks * c + resident - 1) / resident;
-    const double cost = rounds * ((double)len / c + (c > 1 ? extra : 0.0)) * (1.0 + 0.1 / rounds);
+    const double cost = rounds * ((double)len / c + (c > 1 ? extra : 0.0)) * (1.0 + 0.1 / rounds) + (c > 1 ? join : 0.0);
     if (cost < least) { least = cost; best = c; }
     if (rounds > 16) break;
   }
@@ -335,16 +337,18 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   // Rows per workgroup.  Up to 16: the rows kernel, which reads K straight into its products.  More: the step kernel, whose 128 rows meet tiles
   // in LDS; a few of its rows already read at the memory's rate in bf16 (64 sequences of 4000 tokens, 20 rows: 200 us, two passes of 16 rows
   // over the pages 290).  In 4 bits its tiles come by way of registers, one step ahead of another, and the rows kernel with 32 rows is ahead
-  // up to two blocks (20 rows 61 us against 165; 64 rows 130 against 150; few sequences with 40 to 50 rows are up to 12 % behind).
-  p.block_rows = rows <= 16 ? 16 : rows <= 64 && kv->fmt == kMx4 ? 32 : 128;
+  // up to two blocks (20 rows 61 us against 165; 64 rows 130 against 150; few sequences with 40 to 50 rows are up to 12 % behind).  In 8 bits for one
+  // block (20 rows 89 us against 121; 40 rows 167 against 135, 64 rows 186 against 136).
+  p.block_rows = rows <= 16 ? 16 : rows <= (kv->fmt == kMx4 ? 64 : kv->fmt == kMx8 ? 32 : 0) ? 32 : 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
   // tokens that a block sees: all, or the window of its rows and the first tokens
   const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_tokens)) : b->max_len;
   const int64_t len = std::max<int64_t>(1, seen);
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
-  const bool four = kv->fmt == kMx4;
-  p.n_chunks = (int32_t)attend_parts((four && p.block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus, four, blocks, len, per_seq);
+  const auto parts_of = [&](int64_t n) { return (int32_t)attend_parts((kv->fmt == kMx4 && p.block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus, kv->fmt, blocks, n, per_seq); };
+  p.n_chunks = parts_of(len);
+  if (kv->fmt == kMx8 && len < b->max_len) p.n_chunks = std::min(p.n_chunks, parts_of(b->max_len));      // (the workspace has room for so many, whatever the window)
   const int64_t tile = p.block_rows == 128 ? 64 : 32;
   p.piece_tiles = (int32_t)(((len + tile - 1) / tile + p.n_chunks - 1) / p.n_chunks);
   plan_space(p);

@@ -459,9 +459,9 @@ __device__ __forceinline__ void load_tile(const KvDev& kv, const Pages<2>& pg, i
       for (int e = 0; e < 2; ++e) {
         r.k[2 * tt + e] = load_once<u32x4>(k + row0 * kRow8 + (n * kRow8 + 16 * g) + 64 * e);
         r.v[2 * tt + e] = load_once<u32x4>(v + row0 * kRow8 + 16 * lane + 1024 * e);
-        r.ve[2 * tt + e] = load_once<uint8_t>(v + (T * kRow8 + row0 * 4) + (lane >> 1) + 32 * e);
+        r.ve[2 * tt + e] = *reinterpret_cast<const uint8_t*>(v + (T * kRow8 + row0 * 4) + (lane >> 1) + 32 * e);
       }
-      r.ke[tt] = load_once<uint32_t>(k + (T * kRow8 + row0 * 4) + 4 * n);
+      r.ke[tt] = *reinterpret_cast<const uint32_t*>(k + (T * kRow8 + row0 * 4) + 4 * n);
     } else {
       const int64_t base = (((page << kv.page_shift) + row0) * kv.heads + h) * kRow;
       const char* k = kv.k + base + (n * kv.heads * kRow + 16 * g);
@@ -634,7 +634,7 @@ __device__ __forceinline__ void attend_rows(const KvDev kv, const KvAttendDev at
   uint16_t* Vs = reinterpret_cast<uint16_t*>(lds) + wave * kTile * kRowStride;
   // kTurns tiles take turns: once the scores of one are there its registers belong to a later tile, which travels while this one's weights
   // and second products run and the other tiles are worked on.
-  constexpr int kTurns = 2;                  // (three and four: the 4-bit kernel spills and loses 5 and 70 %)
+  constexpr int kTurns = 2;                  // (three and four: the 4-bit kernel spills and loses 5 and 70 %, the 8-bit one gains nothing, and loses 9 %)
   Raw<FMT> raw[kTurns];
   const int first = t_begin + wave;
   PageList<2> pages;

@@ -104,3 +104,18 @@ def test_plain_form_against_softmax():
     v[1] = float("inf")
     out, _, _, _ = ph.attend([(3, 3)], q, k, v, 0.1)
     assert torch.isfinite(out[0]).all() and (out[1:3] == float("inf")).all()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a machine without a GPU is meant")
+def test_the_workspace_of_eight_bit_pages_serves_every_window():
+    from test_kv_args import batch as kv_batch, cache, io as kv_io
+    rng = np.random.default_rng(12)
+    for _ in range(4000):
+        heads, seqs = int(rng.choice([1, 2, 3, 8])), int(2 ** rng.uniform(0, 11))
+        group, length = int(rng.choice([1, 4, 5, 8, 16])), int(2 ** rng.uniform(0, 18))
+        tokens = int(rng.choice([seqs, seqs * 3, seqs + 7, seqs * 40]))
+        kv, qd = make(tdk.KV_MXFP8, num_kv_heads=heads), heads * group * 128
+        b = kv_batch(n_seqs=seqs, n_tokens=tokens, max_len=length)
+        need = tdk.tdk_kv_attend_workspace_bytes(kv, b, heads * group)
+        a = kv_io(n_q_heads=heads * group, q_stride=qd, out_stride=qd, window=int(2 ** rng.uniform(0, 18)), n_sink=int(rng.integers(0, 9)), workspace_bytes=need)
+        refused(lambda: tdk.tdk_kv_attend(kv, cache(), b, a), say="device")
