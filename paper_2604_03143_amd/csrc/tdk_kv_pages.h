@@ -234,7 +234,7 @@ __device__ __forceinline__ bool find_block(const KvDev& kv, const KvAttendDev& a
   b.q0 = min(max(q0, 0), kv.n_tokens);
   const int n = min(max(q1, 0), kv.n_tokens) - b.q0;
   b.n_rows = n * at.group;                   // (at most n_tokens * n_q_heads, which the host has checked)
-  if (n <= 0 || r0 >= b.n_rows) return false;
+  if (n <= 0 || (uint64_t)r0 >= (uint64_t)b.n_rows) return false;       // (negative where the starts decrease)
   b.r0 = (int)r0;
   b.pos0 = max(len, 0) - n;                  // (tokens of a call and of a table are at most 2^30: differences of positions fit)
   b.p_lo = b.pos0 + b.r0 / at.group;

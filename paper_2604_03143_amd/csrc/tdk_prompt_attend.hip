@@ -74,7 +74,7 @@ __device__ __forceinline__ bool find_rows(const KvDev& kv, const PromptAttendDev
   const int n = q1 - b.q0;
   n_keys = max(k1 - k0, 0);
   b.n_rows = n * at.group;
-  if (n <= 0 || r0 < 0 || r0 >= b.n_rows) return false;
+  if (n <= 0 || (uint64_t)r0 >= (uint64_t)b.n_rows) return false;       // (negative where the starts decrease)
   b.r0 = (int)r0;
   b.pos0 = n_keys - n;                       // (negative: the first queries see nothing)
   b.p_lo = b.pos0 + b.r0 / at.group;

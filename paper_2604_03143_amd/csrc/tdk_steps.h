@@ -252,34 +252,31 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
   }
   if (!active) return;
 
-  // The rows go out by way of LDS, where 16 lanes hold one: piece c (16 bytes) of row n stands at place c ^ n.
   float l = st.l_run;
   l += __shfl_xor(l, 32);
-  const int piece = lane & 15;
   if (at.n_chunks == 1 && !at.other_out && !Source::wide(at) && !marks) {
+    const int own = (int)(threadIdx.x & 31), half = (int)(threadIdx.x >> 5 & 1);     // (n and hh, worked out again rather than kept)
+    if (own >= n_on) return;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    const int x = first + (int)(threadIdx.x & 31), t = near_div(at, x);      // (worked out again rather than kept)
-    if (at.lse && hh == 0 && n < n_on) at.lse[(tok0 + t) * at.n_q_heads + h * at.group + x - t * at.group] = l > 0.f ? st.m_run * at.scale + __logf(l * kRaise) : l != l ? l : -INFINITY;
-    char* turn = reinterpret_cast<char*>(&sh) + wave * 32 * kRow;
+    const int x = first + own, t = near_div(at, x), hq = h * at.group + x - t * at.group;
+    if (at.lse && half == 0) at.lse[(tok0 + t) * at.n_q_heads + hq] = l > 0.f ? st.m_run * at.scale + __logf(l * kRaise) : l != l ? l : -INFINITY;
+    char* dst = at.out + (tok0 + t) * at.out_stride + hq * kRow + 16 * half;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<u32x2*>(turn + n * kRow + 16 * ((4 * e + q4) ^ (n & 15)) + 8 * hh) =
-            u32x2{pack2(st.oacc[e][4 * q4] * inv, st.oacc[e][4 * q4 + 1] * inv), pack2(st.oacc[e][4 * q4 + 2] * inv, st.oacc[e][4 * q4 + 3] * inv)};
-    wave_sync();
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int row = 4 * k + (lane >> 4);
-      if (row >= n_on) continue;
-      const int t = near_div(at, first + row);
-      *reinterpret_cast<u32x4*>(at.out + (tok0 + t) * at.out_stride + (h * at.group + first + row - t * at.group) * kRow + 16 * piece) =
-          *reinterpret_cast<const u32x4*>(turn + row * kRow + 16 * (piece ^ (row & 15)));
-    }
+      for (int q4 = 0; q4 < 4; q4 += 2) {
+        // The lane pair of a row has eight elements each of its pieces q4 and q4 + 1 by halves: exchanged, one lane has the one piece, the other the other.
+        const f32x16& o = st.oacc[e];
+        const auto a = __builtin_amdgcn_permlane32_swap(pack2(o[4 * q4] * inv, o[4 * q4 + 1] * inv), pack2(o[4 * q4 + 4] * inv, o[4 * q4 + 5] * inv), false, false);
+        const auto c = __builtin_amdgcn_permlane32_swap(pack2(o[4 * q4 + 2] * inv, o[4 * q4 + 3] * inv), pack2(o[4 * q4 + 6] * inv, o[4 * q4 + 7] * inv), false, false);
+        *reinterpret_cast<u32x4*>(dst + 16 * (4 * e + q4)) = u32x4{a[0], c[0], a[1], c[1]};
+      }
     return;
   }
+  // The rows go out by way of LDS, where 16 lanes hold one: piece c (16 bytes) of row n stands at place c ^ n.
   char* turn = reinterpret_cast<char*>(&sh) + wave * 32 * 4 * kHeadDim;
   static_assert(4 * 32 * 4 * kHeadDim <= sizeof(sh.k) + sizeof(sh.v), "a wavefront's rows lie over the tiles");
+  const int piece = lane & 15;
   const float m = part_max(st.m_run, l);
 #pragma unroll
   for (int e = 0; e < 4; ++e)

@@ -87,7 +87,7 @@ def same(*n):
     return [(x, x) for x in n]
 
 
-# 1000 tokens of 8 heads with 5 queries each are enough rows for the kernel of 256 at a time where there are several sequences
+# enough row blocks of enough sequences that no work is split
 WIDE = same(*[400] * 17)
 
 
@@ -99,9 +99,16 @@ def test_lengths(H, group, lengths):
 
 @pytest.mark.parametrize("H,group,n", [(8, 5, 1111), (8, 1, 2100), (1, 16, 2300), (2, 7, 1900), (8, 16, 700)])
 def test_long_prompts(H, group, n):
-    """Enough rows for 256 at a time, and not."""
+    """A lone prompt, and one of several: its blocks are paired otherwise."""
     check(H, group, same(n))
     check(H, group, same(n, 77, n // 2, 3, n // 3, 900, 800), fused=True)
+
+
+@pytest.mark.parametrize("H,group", [(1, 33), (1, 129), (2, 255), (1, 256), (1, 300), (2, 1000)])
+@pytest.mark.parametrize("lengths", [same(1, 3), same(70), [(5, 200), (1, 1), (33, 40)]])
+def test_more_queries_to_a_head_than_a_block_has_rows(H, group, lengths):
+    check(H, group, lengths, pad_q=1)
+    check(H, group, lengths, window=9, sink=2, join=True)
 
 
 @pytest.mark.parametrize("lengths", [[(1, 1000)], [(5, 1000), (1, 1), (40, 41)], [(64, 4000)], [(300, 900), (20, 20), (700, 1500)], [(1, 30000)]])
