@@ -252,58 +252,74 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
   }
   if (!active) return;
 
+  // A row's two lanes hold it by four elements in turn.
   float l = st.l_run;
   l += __shfl_xor(l, 32);
-  if (at.n_chunks == 1 && !at.other_out && !Source::wide(at) && !marks) {
-    const int own = (int)(threadIdx.x & 31), half = (int)(threadIdx.x >> 5 & 1);     // (n and hh, worked out again rather than kept)
-    if (own >= n_on) return;
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    const int x = first + own, t = near_div(at, x), hq = h * at.group + x - t * at.group;
-    if (at.lse && half == 0) at.lse[(tok0 + t) * at.n_q_heads + hq] = l > 0.f ? st.m_run * at.scale + __logf(l * kRaise) : l != l ? l : -INFINITY;
-    char* dst = at.out + (tok0 + t) * at.out_stride + hq * kRow + 16 * half;
+  const int own = (int)(threadIdx.x & 31), half = (int)(threadIdx.x >> 5 & 1);       // (n and hh, worked out again rather than kept)
+  if (own >= n_on) return;
+  const int x = first + own, t = near_div(at, x), hq = h * at.group + x - t * at.group;
+  const int64_t row = (tok0 + t) * at.n_q_heads + hq;
+  f32x16 (&o)[4] = st.oacc;
+  if (marks) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; q4 += 2) {
-        // The lane pair of a row has eight elements each of its pieces q4 and q4 + 1 by halves: exchanged, one lane has the one piece, the other the other.
-        const f32x16& o = st.oacc[e];
-        const auto a = __builtin_amdgcn_permlane32_swap(pack2(o[4 * q4] * inv, o[4 * q4 + 1] * inv), pack2(o[4 * q4 + 4] * inv, o[4 * q4 + 5] * inv), false, false);
-        const auto c = __builtin_amdgcn_permlane32_swap(pack2(o[4 * q4 + 2] * inv, o[4 * q4 + 3] * inv), pack2(o[4 * q4 + 6] * inv, o[4 * q4 + 7] * inv), false, false);
-        *reinterpret_cast<u32x4*>(dst + 16 * (4 * e + q4)) = u32x4{a[0], c[0], a[1], c[1]};
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t mk = sh.marks[32 * wave + own][16 * e + 4 * (i >> 2) + 2 * half + ((i & 3) >> 1)];
+        o[e][i] = marked(o[e][i], i & 1 ? mk >> 4 : mk & 15u);
       }
+  }
+  const auto four = [&](int e, int q4) __attribute__((always_inline)) { return f32x4{o[e][4 * q4], o[e][4 * q4 + 1], o[e][4 * q4 + 2], o[e][4 * q4 + 3]}; };
+  if (at.n_chunks > 1) {
+    const int64_t part = row * at.n_chunks + chunk;
+    float* dst = at.part_o + part * kHeadDim + 4 * half;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) *reinterpret_cast<f32x4*>(dst + 32 * e + 8 * q4) = four(e, q4);
+    if (half == 0) *reinterpret_cast<f32x2*>(at.part_ml + 2 * part) = f32x2{part_max(st.m_run, l), l};
     return;
   }
-  // The rows go out by way of LDS, where 16 lanes hold one: piece c (16 bytes) of row n stands at place c ^ n.
-  char* turn = reinterpret_cast<char*>(&sh) + wave * 32 * 4 * kHeadDim;
-  static_assert(4 * 32 * 4 * kHeadDim <= sizeof(sh.k) + sizeof(sh.v), "a wavefront's rows lie over the tiles");
-  const int piece = lane & 15;
-  const float m = part_max(st.m_run, l);
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4)
-      *reinterpret_cast<f32x4*>(turn + n * 512 + 16 * ((8 * e + 2 * q4 + hh) ^ n)) =
-          f32x4{st.oacc[e][4 * q4], st.oacc[e][4 * q4 + 1], st.oacc[e][4 * q4 + 2], st.oacc[e][4 * q4 + 3]};
-  wave_sync();
-#pragma clang loop unroll(disable)
-  for (int k = 0; k < 8; ++k) {
-    const int row = 4 * k + (lane >> 4);
-    const float rm = __shfl(m, row), rl = __shfl(l, row);
-    if (row >= n_on) continue;
-    const f32x4 x = *reinterpret_cast<const f32x4*>(turn + row * 512 + 16 * ((2 * piece) ^ row));
-    const f32x4 y = *reinterpret_cast<const f32x4*>(turn + row * 512 + 16 * ((2 * piece + 1) ^ row));
-    float o[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    if (marks) {
+    for (int i = 0; i < 16; ++i) o[e][i] *= inv;
+  float lse = l > 0.f ? st.m_run * at.scale + __logf(l * kRaise) : l != l ? l : -INFINITY;
+  if (at.other_out) {                        // (as in `finish`, all of the row at once)
+    const float pl = at.other_lse[row];
+    if (pl != -INFINITY) {
+      const float* src = at.other_out + row * kHeadDim + 4 * half;
+      f32x4 po[16];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t mk = sh.marks[32 * wave + row][4 * piece + e];
-        o[2 * e] = marked(o[2 * e], mk & 15u);
-        o[2 * e + 1] = marked(o[2 * e + 1], mk >> 4);
-      }
+      for (int k = 0; k < 16; ++k) po[k] = *reinterpret_cast<const f32x4*>(src + 8 * k);
+      const float top = fmaxf(lse, pl);
+      const float w = lse == top ? 1.f : __expf(lse - top), pw = pl == top ? 1.f : __expf(pl - top), both = w + pw, wb = w / both, pb = pw / both;
+#pragma unroll
+      for (int k = 0; k < 64; ++k) o[k >> 4][k & 15] = wb * o[k >> 4][k & 15] + pb * po[k >> 2][k & 3];
+      lse = top + __logf(both);
     }
-    const int t = near_div(at, first + row);
-    put_row(at, tok0 + t, h * at.group + first + row - t * at.group, chunk, piece, o, rm, rl);
   }
+  if (at.lse && half == 0) at.lse[row] = lse;
+  if (Source::wide(at)) {
+    float* dst = reinterpret_cast<float*>(at.out + (tok0 + t) * at.out_stride + hq * (2 * kRow)) + 4 * half;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) *reinterpret_cast<f32x4*>(dst + 32 * e + 8 * q4) = four(e, q4);
+    return;
+  }
+  char* dst = at.out + (tok0 + t) * at.out_stride + hq * kRow + 16 * half;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; q4 += 2) {
+      // Their halves of the pieces q4 and q4 + 1 (16 bytes of bf16) exchanged: one lane has the one piece, the other the other.
+      const f32x4 y = four(e, q4), z = four(e, q4 + 1);
+      const auto a = __builtin_amdgcn_permlane32_swap(pack2(y[0], y[1]), pack2(z[0], z[1]), false, false);
+      const auto c = __builtin_amdgcn_permlane32_swap(pack2(y[2], y[3]), pack2(z[2], z[3]), false, false);
+      *reinterpret_cast<u32x4*>(dst + 16 * (4 * e + q4)) = u32x4{a[0], c[0], a[1], c[1]};
+    }
 }
 
 }  // namespace
