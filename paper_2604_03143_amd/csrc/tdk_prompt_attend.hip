@@ -1,4 +1,6 @@
-// Attention of whole prompts whose rows are not in pages: packed sequences, K and V straight from the projections.
+// Attention of whole prompts whose rows are not in pages: packed sequences, K and V straight from the projections.  The rows of a block are (token, query
+// head of the group) pairs of one sequence and KV head, so that a head's queries share its tiles.  (attend_in_steps has the mathematics and what bounds it.)
+// Every (sequence, KV head) stays on one XCD as far as the launch order decides, whose L2 holds its K and V.
 #include "tdk_steps.h"
 
 namespace tdk {

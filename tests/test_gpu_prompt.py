@@ -197,6 +197,33 @@ def test_random_batches(seed):
     check(H, group, lengths, seed=seed, pad_q=int(rng.integers(0, 4)), pad_k=int(rng.integers(0, 4)), stride_pad=8 * int(rng.integers(0, 3)), join=bool(rng.random() < 0.4), **kw)
 
 
+@pytest.mark.parametrize("n_seqs", [62, 63, 64, 65, 127, 128, 129, 300])
+def test_many_sequences(n_seqs):
+    """As many starts as lanes and more, with sequences that have nothing among them."""
+    lengths = [(0, 3) if s % 7 == 2 else (0, 0) if s % 7 == 4 else (1 + 37 * s % 90, 1 + 37 * s % 90 + (s % 3) * 11) for s in range(n_seqs)]
+    check(2, 5, lengths, pad_q=1, pad_k=1)
+
+
+def test_rows_as_far_apart_as_they_may_be():
+    """Strides of 2^24 elements: a whole step of 64 tokens, and one that ends before."""
+    H, Hq, n, stride = 2, 6, 100, 1 << 24
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (bf(torch.randn(n, h * 128, generator=g)) for h in (Hq, H, H))
+    big = torch.zeros(n * stride - stride + 2 * H * 128, dtype=torch.bfloat16, device="cuda")
+    rows = [big[i * H * 128:].as_strided((n, H * 128), (stride, 1)) for i in (0, 1)]
+    for d, x in zip(rows, (k, v)):
+        d.copy_(x.cuda())
+    dq, s = q.cuda(), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    out, lse = torch.zeros(n, Hq * 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, Hq, device="cuda")
+    kv, batch = tdk.tdk_kv_create(tdk.model(1, H)), tdk.prompt_batch(1, n, n, n, s, s)
+    space = torch.empty(max(256, tdk.tdk_prompt_attend_workspace_bytes(kv, batch, Hq)), dtype=torch.uint8, device="cuda")
+    tdk.tdk_prompt_attend(kv, batch, tdk.prompt_attend_io(dq, Hq * 128, Hq, rows[0], stride, rows[1], stride, 0.09, out, Hq * 128, lse, space, space.numel()), stream())
+    torch.cuda.synchronize()
+    want, wlse, mass, scores = ph.attend([(n, n)], q.double().reshape(n, Hq, 128), k.double().reshape(n, H, 128), v.double().reshape(n, H, 128), 0.09)
+    tol, ltol = kh.tolerance(want, wlse, mass, scores, n)
+    assert far(out.cpu().double().reshape(n, Hq, 128), want, tol) == 0 and far(lse.cpu().double(), wlse, ltol) == 0
+
+
 def test_results_repeat_bit_for_bit():
     for lengths in (same(50, 12), WIDE, [(3, 5000)]):
         first = check(8, 5, lengths)
