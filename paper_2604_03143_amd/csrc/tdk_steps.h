@@ -235,7 +235,8 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
       const int ok = src.ok(1);
       whole = more && src.whole(i + 1);
       // (the tiles that are replaced were used up before the last barrier)
-      src.bring(i, place ^ 1, more && !whole);
+      const bool brings = more || !Source::kEnds;
+      if (brings) src.bring(i, place ^ 1, more && !whole);
       if (active) {
         if (far) {
           const float ref = reference(st.m_run);
@@ -250,9 +251,11 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
         }
         settle(mx);
       }
-      src.arrived(i, place ^ 1, more && !whole);
+      if (brings) {
+        src.arrived(i, place ^ 1, more && !whole);
+        __syncthreads();
+      }
       ++i;
-      __syncthreads();
     };
     while (i < t_end) {
       step(0, s0, s1);
