@@ -51,7 +51,7 @@ struct KvRotateDev {
   char*       q_out;
   int64_t     k_stride, k_out_stride, q_stride, q_out_stride;   // bytes
   int32_t     n_k_heads, n_q_heads;                         // 0: none
-  int32_t     waves;           // workgroups per token
+  int32_t     waves;           // wavefronts per token: in one workgroup (many tokens) or in as many
   int32_t     rotary;
   double      cos_size, sin_size;                           // factors of the cosines and sines
   double      inv_freq[kHalf];

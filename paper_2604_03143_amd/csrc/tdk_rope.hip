@@ -37,15 +37,16 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
 // never crosses lanes.  R elements turn, in pieces of eight: half layout: the lanes c < R / 16 hold the pieces c and c + R / 16, the others two of
 // the pieces behind, which pass as they are; interleaved: pieces c and c + 8, of which those below R / 8 turn.
 // Angles as in the append: one per lane, in double, rounded to fp32 once; a pair turns in fp32 and is rounded to bf16 once.
-// What bounds it: memory.  12 333 tokens (8 + 40 heads): 51 us, 5.9 TB/s; 32 768: 129 us, 6.2 TB/s; reads and writes pass the caches by.  Four tokens: 3.7 us, of which the launch
-// is most.  Four wavefronts share a token's angles where there are many (many_rows); few tokens have a workgroup for each eight heads.
+// What bounds it: memory.  12 333 tokens (8 + 40 heads): 51 us, 5.9 TB/s; 32 768: 129 us, 6.2 TB/s; 40 000 with 24 heads, half of each: 75 us, 5.9 TB/s; reads and writes pass the caches by.  Four tokens: 3.7 us, of which the launch
+// is most.  Up to four wavefronts, one for each eight heads, share a token's angles where there are many tokens (many_rows; always four: 16 heads 66 us for 51); few
+// tokens have a workgroup for each eight heads.
 // ---------------------------------------------------------------------------------------------
-template <bool ONCE>
-__global__ __launch_bounds__(ONCE ? 256 : 64) void tdk_kv_rotate_kernel(const KvDev kv, const KvRotateDev r) {
+template <bool MANY, bool ONCE>
+__global__ __launch_bounds__(MANY ? 256 : 64) void tdk_kv_rotate_kernel(const KvDev kv, const KvRotateDev r) {
   __shared__ float2 turn[kHalf];
   const int lane = threadIdx.x & 63, c = lane & 7, hl = lane >> 3;
-  const int row = ONCE ? blockIdx.x : blockIdx.x / r.waves, part = ONCE ? threadIdx.x >> 6 : blockIdx.x - row * r.waves;
-  const int parts = ONCE ? 4 : r.waves;
+  const int row = MANY ? blockIdx.x : blockIdx.x / r.waves, part = MANY ? threadIdx.x >> 6 : blockIdx.x - row * r.waves;
+  const int parts = r.waves;
   const int H = r.n_k_heads, n = H + r.n_q_heads;
   const int R16 = r.rotary >> 4;
   const int pa = kv.interleaved ? c : c < R16 ? c : R16 + c, pb = kv.interleaved ? c + 8 : c < R16 ? c + R16 : 8 + c;
@@ -64,8 +65,8 @@ __global__ __launch_bounds__(ONCE ? 256 : 64) void tdk_kv_rotate_kernel(const Kv
   load(part, na, nb);
   const Slot o = slot_of(kv, row, lane);
   if (o.pos < 0) return;
-  if (!ONCE || part == 0) turn[lane] = angle_of(o.pos, r.inv_freq[lane], r.cos_size, r.sin_size);
-  if (ONCE) __syncthreads();
+  if (!MANY || part == 0) turn[lane] = angle_of(o.pos, r.inv_freq[lane], r.cos_size, r.sin_size);
+  if (MANY) __syncthreads();
   else wave_sync();
   float2 t[8];
 #pragma unroll
@@ -209,8 +210,11 @@ __global__ __launch_bounds__(64) void tdk_kv_append_rope_kernel(const KvDev kv, 
   }
 }
 
+// (Half layout, part of the head: the pieces are not whole cache lines, which past the caches would travel twice: 40 000 tokens, 24 heads, 64 of 128: 92 us,
+// through the caches 84; 16 of 128: 98 and 83.)
 hipError_t launch_kv_rotate(const KvDev& kv, const KvRotateDev& r, bool many, hipStream_t st) {
-  return launch(many ? tdk_kv_rotate_kernel<true> : tdk_kv_rotate_kernel<false>, (int64_t)kv.n_tokens * r.waves, many ? 256 : 64, st, kv, r);
+  if (!many) return launch(tdk_kv_rotate_kernel<false, false>, (int64_t)kv.n_tokens * r.waves, 64, st, kv, r);
+  return launch(kv.interleaved || r.rotary == kHeadDim ? tdk_kv_rotate_kernel<true, true> : tdk_kv_rotate_kernel<true, false>, kv.n_tokens, 64 * r.waves, st, kv, r);
 }
 
 hipError_t launch_kv_append_rope(const KvDev& kv, const KvRowsDev& rows, int fmt, bool many, hipStream_t st) {

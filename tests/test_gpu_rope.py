@@ -100,6 +100,13 @@ def test_rotate_many_tokens_and_head_counts(H, Hq, lengths, interleaved, rotary)
     check_rotate(H, Hq, 1e4, interleaved, rotary, TURNS, lengths, fused=True)
 
 
+@pytest.mark.parametrize("H,Hq", [(1, 1), (4, 4), (4, 10), (8, 16), (3, 28), (8, 33)])
+@pytest.mark.parametrize("interleaved,rotary", [(False, 16), (False, 112), (False, 128), (True, 48)])
+def test_rotate_many_tokens_with_one_wavefront_each_to_four(H, Hq, interleaved, rotary):
+    check_rotate(H, Hq, 1e4, interleaved, rotary, TURNS, [(7, 1300), (0, 1), (2, 900)], pad=1)
+    check_rotate(H, Hq, 1e4, interleaved, rotary, TURNS, [(7, 1300), (2, 900)], in_place=True, fused=True)
+
+
 def test_rotate_leaves_tokens_without_a_position_alone():
     def spoil(b):
         b.lens[1] = 1                 # two tokens announced, one long: the first has no position

@@ -19,7 +19,7 @@ def test_no_scratch_and_the_residency_that_calls_are_cut_for(kernels):      # no
 
 def test_rows_have_no_scratch(kernels):      # noqa: F811
     some = dict(forms(kernels, kv8_read={}, kv_rotate={}, kv_append_rope={}))
-    assert len(some) == 2 + 2 + 6
+    assert len(some) == 2 + 3 + 6
     assert not {k: v for k, v in some.items() if v[1]}
 
 
