@@ -7,6 +7,8 @@ namespace tdk {
 
 namespace {
 
+using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
+
 // One thread's share of the loads of a step's tile, rows `stride` bytes apart: piece t % 16 of rows t / 16, 16 + t / 16, ...
 struct RowLoader {
   uint32_t stride, off;
@@ -163,14 +165,18 @@ struct RowSource {
   __device__ __forceinline__ void check_v(int i, int place) const {
     const int j0 = steps.token(i);
     u32x4* own = reinterpret_cast<u32x4*>(sh->v[place] + 16 * threadIdx.x);
-    bool mine = false;
+    u16x2 top = {0, 0};                      // the largest magnitudes, as bits: infinity and NaN are above all that is finite
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const u32x4 x = own[256 * e];
-      if (!one_sees(*a, *blk, j0 + 16 * e + (int)(threadIdx.x >> 4))) own[256 * e] = u32x4{0, 0, 0, 0};
-      else mine |= odd16(x[0]) || odd16(x[1]) || odd16(x[2]) || odd16(x[3]);
+      if (!one_sees(*a, *blk, j0 + 16 * e + (int)(threadIdx.x >> 4))) {
+        own[256 * e] = u32x4{0, 0, 0, 0};
+        continue;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[k] & 0x7fff7fffu));
     }
-    const int any = __any(mine);
+    const int any = __any(max((int)top[0], (int)top[1]) >= 0x7f80);
     if (lane == 0) sh->odd[place][wave] = any;
   }
   __device__ __forceinline__ void first() const {

@@ -139,13 +139,17 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
   {
     const bool on = n < n_on;
     const char* q = at.q + (on ? tok0 + my_tok : b.q0) * at.q_stride + (on ? h * at.group + first + n - my_tok * at.group : 0) * kRow;
+    u32x4 x[8];                              // (rows that there are not: as the block's first, and not written)
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      u32x4 x = *reinterpret_cast<const u32x4*>(q + 32 * kk + 16 * hh);
+    for (int kk = 0; kk < 8; ++kk) x[kk] = *reinterpret_cast<const u32x4*>(q + 32 * kk + 16 * hh);
+    if (at.q_flip) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = on ? (at.q_flip ? x[e] ^ 0x80008000u : x[e]) : 0u;
-      qf[kk] = __builtin_bit_cast(bf16x8, x);
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[kk][e] ^= 0x80008000u;
     }
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) qf[kk] = __builtin_bit_cast(bf16x8, x[kk]);
   }
   RowState st;
   row_state_init(st);
