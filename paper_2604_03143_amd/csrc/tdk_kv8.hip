@@ -33,17 +33,18 @@ struct PageSource {
   PageList<4> pages;
   Codes8 ck, cv;
   int h, t_begin, t_end, wave, lane;
-  __device__ __forceinline__ Codes8 fetch(const char* plane, const Pages<4>& pg) const {
-    const int T = 1 << cache->page_shift;
-    const int64_t page = max(wave == 0 ? pg.p[0] : wave == 1 ? pg.p[1] : wave == 2 ? pg.p[2] : pg.p[3], 0);
-    const int row0 = 16 * wave & (T - 1);
+  // of the d-th step behind the current one
+  __device__ __forceinline__ Codes8 fetch(const char* plane, int d) const {
+    const int T = 1 << cache->page_shift, row0 = 16 * wave & (T - 1);
+    const int64_t page = max(pages.get(d, wave), 0);
     const char* base = plane + (page * cache->heads + h) * (T * (kRow8 + 4));
+    const char *c = base + row0 * kRow8, *e = base + (T * kRow8 + row0 * 4);
+    const uint32_t off = 16u * (uint32_t)lane, off_e = (uint32_t)lane >> 1;
     Codes8 x;
-    x.c[0] = *reinterpret_cast<const u32x4*>(base + row0 * kRow8 + 16 * lane);
-    x.c[1] = *reinterpret_cast<const u32x4*>(base + row0 * kRow8 + 1024 + 16 * lane);
-    const char* e = base + (T * kRow8 + row0 * 4) + (lane >> 1);
-    x.e[0] = *reinterpret_cast<const uint8_t*>(e);
-    x.e[1] = *reinterpret_cast<const uint8_t*>(e + 32);
+    x.c[0] = *reinterpret_cast<const u32x4*>(c + off);
+    x.c[1] = *reinterpret_cast<const u32x4*>(c + off + 1024);
+    x.e[0] = *reinterpret_cast<const uint8_t*>(e + off_e);
+    x.e[1] = *reinterpret_cast<const uint8_t*>(e + off_e + 32);
     return x;
   }
   template <bool V>
@@ -101,10 +102,10 @@ struct PageSource {
   }
   __device__ __forceinline__ bool whole(int i) const { return seen(i, ok(i == t_begin ? 0 : 1)); }
   __device__ __forceinline__ void first() {
-    const Codes8 k0 = fetch(cache->k, pages.get(0)), k1 = fetch(cache->k, pages.get(1));
-    Codes8 v0 = fetch(cache->v, pages.get(0));
-    ck = fetch(cache->k, pages.get(2));
-    cv = fetch(cache->v, pages.get(1));
+    const Codes8 k0 = fetch(cache->k, 0), k1 = fetch(cache->k, 1);
+    Codes8 v0 = fetch(cache->v, 0);
+    ck = fetch(cache->k, 2);
+    cv = fetch(cache->v, 1);
     put<false>(k0, sh->k[1]);
     const int there0 = ok(0);
     if (!seen(t_begin, there0)) check(t_begin, there0, 0, v0);
@@ -115,8 +116,8 @@ struct PageSource {
     put<false>(ck, sh->k[place]);
     if (to_check) check(i + 1, ok(1), place, cv);
     put<true>(cv, sh->v[place]);
-    ck = fetch(cache->k, pages.get(3));
-    cv = fetch(cache->v, pages.get(2));
+    ck = fetch(cache->k, 3);
+    cv = fetch(cache->v, 2);
     pages.next(*cache, blk->s, tiles, t_begin, 1, t_end, lane);
   }
   __device__ __forceinline__ void arrived(int, int, bool) const {}

@@ -409,6 +409,10 @@ struct PageList {
     for (int it = 0; it < N; ++it) o.p[it] = __builtin_amdgcn_readlane(r, l + it);
     return o;
   }
+  __device__ __forceinline__ int get(int d, int it) const {    // one of them
+    const int k = at + d;
+    return __builtin_amdgcn_readlane(k < kTiles ? now : then, (k < kTiles ? k : k - kTiles) * N + it);
+  }
 };
 
 template <int N>
