@@ -33,6 +33,7 @@ struct PageSource {
   PageList<4> pages;
   Codes8 ck, cv;
   int h, t_begin, t_end, wave, lane;
+  uint32_t put_k, put_v;                     // the first of the lane's places in a tile
   // of the d-th step behind the current one
   __device__ __forceinline__ Codes8 fetch(const char* plane, int d) const {
     const int T = 1 << cache->page_shift, row0 = 16 * wave & (T - 1);
@@ -49,17 +50,13 @@ struct PageSource {
   }
   template <bool V>
   __device__ __forceinline__ void put(const Codes8& x, unsigned char* tile) const {
-    int ln = lane;
-    asm volatile("" : "+v"(ln));             // (the places in the tiles are worked out again: kept from step to step they spill)
+    uint32_t at = V ? put_v : put_k;
+    asm volatile("" : "+v"(at));             // (the other places are worked out from the first: kept from step to step they spill)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int t = 16 * wave + 8 * i + (ln >> 3);
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = 2 * (ln & 7) + e;
-        *reinterpret_cast<u32x4*>(tile + (V ? v_place(t, c) : k_place(t, c))) = from8(x.c[i][2 * e], x.c[i][2 * e + 1], x.e[i]);
-      }
-    }
+      for (int e = 0; e < 2; ++e)            // (token + 8: K's rows place their pieces by four bits of it, V's by two)
+        *reinterpret_cast<u32x4*>(tile + ((at ^ (16 * e) ^ (V ? 0 : 128 * i)) + 2048 * i)) = from8(x.c[i][2 * e], x.c[i][2 * e + 1], x.e[i]);
   }
   // V of a step that some rows see and some do not, before it is put there: what none sees becomes zero (a weight of zero would not silence infinity
   // or NaN), and the tile's flag says whether what is left is finite.
@@ -91,6 +88,8 @@ struct PageSource {
     t_end = end;
     lane = lane_;
     wave = wave_;
+    put_k = (uint32_t)k_place(16 * wave + (lane >> 3), 2 * (lane & 7));
+    put_v = (uint32_t)v_place(16 * wave + (lane >> 3), 2 * (lane & 7));
     // (Behind the last step the last one's pages are read again: what that gives is not used.)
     if (begin < end) pages.start(kv, b.s, tiles, begin, 1, end, lane);
   }
