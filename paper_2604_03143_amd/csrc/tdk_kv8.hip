@@ -32,14 +32,14 @@ struct PageSource {
   StepTiles* sh;
   PageList<4> pages;
   Codes8 ck, cv;
-  int h, t_begin, t_end, wave, lane;
+  int t_begin, t_end, wave, lane;
+  const char *codes_k, *codes_v;             // of page 0: the wavefront's tokens
+  uint32_t page_bytes, powers;               // powers: where they stand behind the codes
   uint32_t put_k, put_v;                     // the first of the lane's places in a tile
   // of the d-th step behind the current one
   __device__ __forceinline__ Codes8 fetch(const char* plane, int d) const {
-    const int T = 1 << cache->page_shift, row0 = 16 * wave & (T - 1);
-    const int64_t page = max(pages.get(d, wave), 0);
-    const char* base = plane + (page * cache->heads + h) * (T * (kRow8 + 4));
-    const char *c = base + row0 * kRow8, *e = base + (T * kRow8 + row0 * 4);
+    const char* c = plane + (uint64_t)(uint32_t)max(pages.get(d, wave), 0) * page_bytes;
+    const char* e = c + powers;
     const uint32_t off = 16u * (uint32_t)lane, off_e = (uint32_t)lane >> 1;
     Codes8 x;
     x.c[0] = *reinterpret_cast<const u32x4*>(c + off);
@@ -83,11 +83,15 @@ struct PageSource {
     a = &at;
     blk = &b;
     sh = &to;
-    h = head;
     t_begin = begin;
     t_end = end;
     lane = lane_;
     wave = wave_;
+    const int T = 1 << kv.page_shift, row0 = 16 * wave & (T - 1);
+    page_bytes = (uint32_t)(kv.heads * T * (kRow8 + 4));
+    powers = (uint32_t)(T * kRow8 + row0 * 4 - row0 * kRow8);
+    codes_k = kv.k + (int64_t)head * (T * (kRow8 + 4)) + row0 * kRow8;
+    codes_v = kv.v + (int64_t)head * (T * (kRow8 + 4)) + row0 * kRow8;
     put_k = (uint32_t)k_place(16 * wave + (lane >> 3), 2 * (lane & 7));
     put_v = (uint32_t)v_place(16 * wave + (lane >> 3), 2 * (lane & 7));
     // (Behind the last step the last one's pages are read again: what that gives is not used.)
@@ -101,10 +105,10 @@ struct PageSource {
   }
   __device__ __forceinline__ bool whole(int i) const { return seen(i, ok(i == t_begin ? 0 : 1)); }
   __device__ __forceinline__ void first() {
-    const Codes8 k0 = fetch(cache->k, 0), k1 = fetch(cache->k, 1);
-    Codes8 v0 = fetch(cache->v, 0);
-    ck = fetch(cache->k, 2);
-    cv = fetch(cache->v, 1);
+    const Codes8 k0 = fetch(codes_k, 0), k1 = fetch(codes_k, 1);
+    Codes8 v0 = fetch(codes_v, 0);
+    ck = fetch(codes_k, 2);
+    cv = fetch(codes_v, 1);
     put<false>(k0, sh->k[1]);
     const int there0 = ok(0);
     if (!seen(t_begin, there0)) check(t_begin, there0, 0, v0);
@@ -115,8 +119,8 @@ struct PageSource {
     put<false>(ck, sh->k[place]);
     if (to_check) check(i + 1, ok(1), place, cv);
     put<true>(cv, sh->v[place]);
-    ck = fetch(cache->k, 3);
-    cv = fetch(cache->v, 2);
+    ck = fetch(codes_k, 3);
+    cv = fetch(codes_v, 2);
     pages.next(*cache, blk->s, tiles, t_begin, 1, t_end, lane);
   }
   __device__ __forceinline__ void arrived(int, int, bool) const {}
