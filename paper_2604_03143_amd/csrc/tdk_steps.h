@@ -100,12 +100,12 @@ __device__ __forceinline__ void step_of_rows(const unsigned char* Ks, const unsi
 // A row's weights are 2^(c (s - m) - 12), s its scores, c the scale times log2 e, m a reference point that follows their maximum only from 2^11.5 on, so that
 // sums and products (both fp32) are seldom scaled again; weights go to the second products as bf16 (half a step of 2^-8 each, the error that is left).
 // What bounds it: the clock that matrix and vector units share under load.  A prompt of 8192 tokens, 8 heads with 5 queries each: 613 us, 1121 TFLOP/s of what the
-// queries see where a matrix product of 16 384 reaches 1364; counters: matrix cores 64 % busy, vector units 55 %, 1.7 GHz, no bank conflicts.
+// queries see where a matrix product of 16 384 reaches 1364; counters: matrix cores 65 % busy, vector units 55 %, 1.7 GHz, no bank conflicts.
 // Why so: two workgroups of four wavefronts on a compute unit, 32 rows a wavefront.  64 rows a wavefront spill (1175 us for 720 at the time), eight
 // wavefronts a workgroup wait for one another (676 for 660, 25 short prompts 158 for 138).  Steps that every row sees whole skip all tests by
 // one scalar; the maxima of the next scores stand in the slots of the second products (719 -> 663 us with scalar borders, 655 with that scalar).
 // Tried without gain: sums by dot products (689 for 680) or by a product with ones (640 for 610), no raised priority (628 for 610), loads in the
-// slots, operands three or six ahead.  Of a short prompt's workgroup (16 us) half is start and end: starts 0.9, tiles 2.6, first scores 1.4.
+// slots, operands three or six ahead.  Of a short prompt's workgroup (14 us) half is start and end: starts 0.9, tiles 2.6, first scores 1.4.
 template <class Source>
 __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename Source::At at) {
   __shared__ __align__(16) StepTiles sh;
