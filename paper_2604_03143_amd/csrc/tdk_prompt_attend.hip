@@ -165,22 +165,26 @@ struct RowSource {
   __device__ __forceinline__ void check_v(int i, int place) const {
     const int j0 = steps.token(i);
     u32x4* own = reinterpret_cast<u32x4*>(sh->v[place] + 16 * threadIdx.x);
+    u32x4 x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = own[256 * e];
     u16x2 top = {0, 0};                      // the largest magnitudes, as bits: infinity and NaN are above all that is finite
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const u32x4 x = own[256 * e];
-      if (!one_sees(*a, *blk, j0 + 16 * e + (int)(threadIdx.x >> 4))) {
-        own[256 * e] = u32x4{0, 0, 0, 0};
-        continue;
-      }
+      const int j = j0 + 16 * e + (int)(threadIdx.x >> 4);
+      const bool seen = (j <= blk->p_hi) & ((a->window == 0) | (blk->p_lo - j < a->window) | (j < a->n_sink));
+      const uint32_t size = seen ? 0x7fff7fffu : 0u;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[k] & 0x7fff7fffu));
+      for (int k = 0; k < 4; ++k) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e][k] & size));
+      if (!seen) own[256 * e] = u32x4{0, 0, 0, 0};
     }
     const int any = __any(max((int)top[0], (int)top[1]) >= 0x7f80);
     if (lane == 0) sh->odd[place][wave] = any;
   }
   __device__ __forceinline__ void first() const {
     landed();
+    // The queries are there by now too, and the compiler has to see it: else it waits for their registers in the loop, and so for the tiles on their way.
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
     if (!whole(t_begin)) check_v(t_begin, 0);
   }
   __device__ __forceinline__ void bring(int i, int place, bool) const {

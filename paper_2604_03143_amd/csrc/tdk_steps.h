@@ -35,6 +35,18 @@ __device__ __forceinline__ int near_div(const KvAttendDev& at, int x) {
   return at.group >= 256 ? (x >= at.group ? 1 : 0) : (int)(((uint32_t)x * at.group_inv) >> 22);
 }
 
+// a lane's maximum of a step's scores (NaN where there is one)
+__device__ __forceinline__ float max_of(const f32x16 (&s)[2]) {
+  float a = s[0][0], b = s[1][0];
+#pragma unroll
+  for (int i = 1; i < 15; i += 2) {
+    a = __builtin_elementwise_maximum(a, __builtin_elementwise_maximum(s[0][i], s[0][i + 1]));
+    b = __builtin_elementwise_maximum(b, __builtin_elementwise_maximum(s[1][i], s[1][i + 1]));
+    asm("" : "+v"(a), "+v"(b));
+  }
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, s[0][15]), __builtin_elementwise_maximum(b, s[1][15]));
+}
+
 // The pipelined step of rows_step (tdk_tiles.h), with the maxima kept in their slots: the scores of the next step's K tile, this step's weights, and the
 // products of this step's V tile.  m2: what goes to the scaled scores; mx: each lane's maximum of the new ones.
 __device__ __forceinline__ void step_of_rows(const unsigned char* Ks, const unsigned char* Vs, const bf16x8 (&qf)[8], f32x16 (&s)[2], f32x16 (&nx)[2],
@@ -176,7 +188,7 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
         s[k >> 4][k & 15] = !(t >= hb && t < he) && (ok >> (t >> 4) & 1) ? s[k >> 4][k & 15] : -INFINITY;
       }
     }
-    rows_max<2>(s, mx);
+    mx = max_of(s);
   };
   constexpr float kFar = 4096.f;             // (as in attend_steps: reference points beyond are subtracted before scaling)
   bool far = false, marks = false;
@@ -200,8 +212,8 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
     if (active) {
       float mx;
       rows_scores(sh.k[1], qf, n, hh, s0);
-      rows_max<2>(s0, mx);
-      if (!whole) mask_scores(src.token(t_begin), src.ok(0), s0, mx);
+      if (whole) mx = max_of(s0);
+      else mask_scores(src.token(t_begin), src.ok(0), s0, mx);
       const float m = pair_max(mx);
       st.m_run = m > -INFINITY ? m : -INFINITY;        // (a NaN: as if there were no score yet)
       far = __any(fabsf(reference(st.m_run)) * at.scale2 > kFar);
