@@ -12,6 +12,8 @@ struct Codes8 {
   uint32_t e[2];                             // their exponents
 };
 
+constexpr uint32_t kWide8 = 247;             // from this power on a block's values may be infinite
+
 struct PageSource {
   using At = KvAttendDev;
   static constexpr bool kHoles = true, kSpread = false, kEnds = false;      // (a test whether there is a next step: 40 rows 132 -> 148 us)
@@ -61,21 +63,21 @@ struct PageSource {
   // V of a step that some rows see and some do not, before it is put there: what none sees becomes zero (a weight of zero would not silence infinity
   // or NaN), and the tile's flag says whether what is left is finite.
   __device__ __forceinline__ void check(int i, int there, int place, Codes8& x) const {
-    const int j0 = tiles.tile(i) * kStep;
-    bool mine = false;
+    const int j0 = tiles.tile(i) * kStep, near = a->window ? a->window : INT32_MAX;
+    uint32_t nan = 0, power = 0;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      if (!((there >> wave & 1) && one_sees(*a, *blk, j0 + 16 * wave + 8 * k + (lane >> 3)))) {
-        x.c[k] = u32x4{0, 0, 0, 0};
-        x.e[k] = 0;
-      }
+      const int j = j0 + 16 * wave + 8 * k + (lane >> 3);
+      const bool seen = (there >> wave & 1) & (j <= blk->p_hi) & ((blk->p_lo - j < near) | (j < a->n_sink)) & !((j >= blk->hole_b) & (j < blk->hole_e));
+      x.e[k] = seen ? x.e[k] : 0;
+      power = max(power, x.e[k]);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const u32x4 v = from8(x.c[k][2 * e], x.c[k][2 * e + 1], x.e[k]);
-        mine |= odd16(v[0]) || odd16(v[1]) || odd16(v[2]) || odd16(v[3]);
+      for (int e = 0; e < 4; ++e) {
+        x.c[k][e] = seen ? x.c[k][e] : 0;
+        nan |= (x.c[k][e] & 0x7f7f7f7fu) + 0x01010101u;       // bit 7 of a byte: its code is NaN
       }
     }
-    const int any = __any(mine);
+    const int any = __any((nan & 0x80808080u) != 0 || power >= kWide8);
     if (lane == 0) sh->odd[place][wave] = any;
   }
   __device__ __forceinline__ void open(const KvDev& kv, const At& at, const Block& b, int head, int begin, int end, StepTiles& to, int lane_, int wave_) {
@@ -103,7 +105,7 @@ struct PageSource {
     const int j0 = token(i);
     return there == 15 && all_see(*a, *blk, j0, j0 + kStep - 1);
   }
-  __device__ __forceinline__ bool whole(int i) const { return seen(i, ok(i == t_begin ? 0 : 1)); }
+  __device__ __forceinline__ bool whole(int i, int d) const { return seen(i, ok(d)); }
   __device__ __forceinline__ void first() {
     const Codes8 k0 = fetch(codes_k, 0), k1 = fetch(codes_k, 1);
     Codes8 v0 = fetch(codes_v, 0);

@@ -147,7 +147,7 @@ struct RowSource {
   }
   __device__ __forceinline__ int token(int i) const { return steps.token(i); }
   __device__ __forceinline__ int ok(int) const { return 15; }
-  __device__ __forceinline__ bool whole(int i) const {
+  __device__ __forceinline__ bool whole(int i, int) const {
     const int j0 = steps.token(i);
     return (j0 + kStep - 1 <= blk->p_lo) & ((a->window == 0) | (blk->p_hi - j0 < a->window));
   }
@@ -185,7 +185,7 @@ struct RowSource {
     landed();
     // The queries are there by now too, and the compiler has to see it: else it waits for their registers in the loop, and so for the tiles on their way.
     __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
-    if (!whole(t_begin)) check_v(t_begin, 0);
+    if (!whole(t_begin, 0)) check_v(t_begin, 0);
   }
   __device__ __forceinline__ void bring(int i, int place, bool) const {
     if (i + 2 < t_end) fetch_k(i + 2, place);

@@ -207,7 +207,7 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
   if (t_begin < t_end) {
     f32x16 s0[2], s1[2];
     src.first();
-    bool whole = src.whole(t_begin);         // every row sees all of this step, and no page is missing
+    bool whole = src.whole(t_begin, 0);         // every row sees all of this step, and no page is missing
     __syncthreads();
     if (active) {
       float mx;
@@ -249,7 +249,7 @@ __device__ __forceinline__ void attend_in_steps(const KvDev kv, const typename S
       }
       const bool more = i + 1 < t_end;
       const int ok = src.ok(1);
-      whole = more && src.whole(i + 1);
+      whole = more && src.whole(i + 1, 1);
       // (the tiles that are replaced were used up before the last barrier)
       const bool brings = more || !Source::kEnds;
       if (brings) src.bring(i, place ^ 1, more && !whole);
