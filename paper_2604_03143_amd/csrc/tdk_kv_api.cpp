@@ -338,7 +338,7 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   // in LDS; a few of its rows already read at the memory's rate in bf16 (64 sequences of 4000 tokens, 20 rows: 200 us, two passes of 16 rows
   // over the pages 290).  In 4 bits its tiles come by way of registers, one step ahead of another, and the rows kernel with 32 rows is ahead
   // up to two blocks (20 rows 61 us against 165; 64 rows 130 against 150; few sequences with 40 to 50 rows are up to 12 % behind).  In 8 bits for one
-  // block (20 rows 88 us against 109; 40 rows 172 against 123, 64 rows 186 against 124).
+  // block (20 rows 88 us against 109; 40 rows 172 against 118, 64 rows 186 against 120).
   p.block_rows = rows <= 16 ? 16 : rows <= (kv->fmt == kMx4 ? 64 : kv->fmt == kMx8 ? 32 : 0) ? 32 : 128;
   p.forward = per_seq <= p.block_rows;
   p.ids = (int64_t)b->n_tokens * group / p.block_rows + b->n_seqs;
