@@ -505,7 +505,8 @@ tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
  *              time (two streams, two graphs) need one each
  * Any scale up to 2^127 in magnitude is taken, zero and denormal ones as they are (scores q . K beyond fp32 are infinite
  * before they are scaled; a query all of whose scores are minus infinity counts as one that sees nothing).  What a query
- * does not see does not reach its result, whatever it holds (NaN and infinities included).  bf16 products with fp32 sums;
+ * does not see does not reach its result, whatever it holds (NaN and infinities included).  What it does see does: a NaN in V makes its element
+ * NaN, an infinity makes it infinite, or NaN where the weight is below fp32's range.  bf16 products with fp32 sums;
  * the softmax weights are rounded to bf16 for the second product, their sum is not.  Allocates nothing, one or two
  * kernels, does not synchronise; results do not depend on what else runs. */
 typedef struct {

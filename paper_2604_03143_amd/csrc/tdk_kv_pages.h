@@ -1136,10 +1136,13 @@ __device__ __forceinline__ void join_parts(const KvDev kv, const At at, int64_t 
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (64 * k >= at.n_chunks) break;
-    const float f = m[k] == -INFINITY ? 0.f : share(m[k], top, at.scale2);
+    const bool held = m[k] != -INFINITY;
+    const uint64_t parts_held = __ballot(held);
+    const float f = held ? share(m[k], top, at.scale2) : 0.f;
     sum += f * l[k];
     for (int c0 = 0; c0 < 64 && 64 * k + c0 < at.n_chunks; c0 += 16) {
-      // sixteen parts a time, four of them in each lane's hands: their reads are under way together (parts with no weight are not read)
+      // Sixteen parts a time, four of them in each lane's hands: their reads are under way together.  Parts of which the row saw nothing are not
+      // read (nothing was written there); one whose share is below fp32's range is, so that NaN and infinities in it are not lost.
       f32x4 x[4], y[4];
       float w[4];
 #pragma unroll
@@ -1147,7 +1150,7 @@ __device__ __forceinline__ void join_parts(const KvDev kv, const At at, int64_t 
         const int c = c0 + 4 * u + (lane >> 4);
         w[u] = __shfl(f, c);
         x[u] = y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (w[u] == 0.f) continue;
+        if (!(parts_held >> c & 1)) continue;
         x[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4)];
         y[u] = parts[(int64_t)(64 * k + c) * (kHeadDim / 4) + 1];
       }
