@@ -431,7 +431,7 @@ typedef struct {
  * checked there: starts are cut to [0, n_tokens], and a token whose position is negative, whose logical page
  * lies past table_stride or whose page number is not in [0, pool_pages) is not written by append, reads as zero
  * and is seen by no query.  At most 2^30 sequences, 2^30 tokens per sequence by its table, and per call what one launch
- * holds: 2^32 threads, 256 for each token that is appended or read (else UNSUPPORTED). */
+ * holds: 2^32 threads, 256 for each token that is appended, read or rotated (else UNSUPPORTED). */
 typedef struct {
   int32_t        n_seqs;
   int32_t        n_tokens;

@@ -182,7 +182,7 @@ tdk_status rotate_rows(const tdk_kv* kv, const tdk_kv_batch* b, const tdk_kv_rot
   const int steps = rows_steps(r.n_k_heads + r.n_q_heads);
   const bool many = many_rows(kv, b, steps);
   r.waves = many ? std::max(1, std::min(steps, 4)) : steps;
-  if ((int64_t)b->n_tokens * r.waves * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");
+  if ((int64_t)b->n_tokens * 256 > kMaxThreads) return fail(TDK_ERR_UNSUPPORTED, "batch: more tokens than a launch holds");      // (four wavefronts a token at most where there are many)
   r.rotary = kv->rotary;
   r.cos_size = a->back ? 1.0 / kv->magnitude : kv->magnitude;
   r.sin_size = a->back ? -r.cos_size : r.cos_size;
