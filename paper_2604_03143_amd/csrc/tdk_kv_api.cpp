@@ -322,7 +322,8 @@ void attend_dev(const tdk_kv* kv, const Shared& a, const KvAttendPlan& p, KvAtte
   at.scale2 = at.scale * 1.4426950408889634f;
 }
 
-// window, n_sink: as in the call; without a window the plan is the one with the most parts.  false: bad arguments
+// window, n_sink: as in the call; without a window the plan is the one with the most parts (attend_parts' cost of c parts is a(c) len + b(c), and
+// b never falls with c: a shorter length never gains from more).  false: bad arguments
 bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, int32_t window, int32_t n_sink, KvAttendPlan& p) {
   const int32_t H = kv->model.num_kv_heads;
   if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_len < 0 || n_q_heads < 1 || n_q_heads % H || n_q_heads > kMaxQHeads) return false;
@@ -346,9 +347,7 @@ bool attend_plan_kv(const tdk_kv* kv, const tdk_kv_batch* b, int32_t n_q_heads, 
   const int64_t seen = window > 0 ? std::min<int64_t>(b->max_len, (int64_t)window + n_sink + std::min<int64_t>(p.block_rows / group, b->n_tokens)) : b->max_len;
   const int64_t len = std::max<int64_t>(1, seen);
   const int64_t blocks = (per_seq + p.block_rows - 1) / p.block_rows * b->n_seqs * H;
-  const auto parts_of = [&](int64_t n) { return (int32_t)attend_parts((kv->fmt == kMx4 && p.block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus, kv->fmt, blocks, n, per_seq); };
-  p.n_chunks = parts_of(len);
-  if (kv->fmt == kMx8 && len < b->max_len) p.n_chunks = std::min(p.n_chunks, parts_of(b->max_len));      // (the workspace has room for so many, whatever the window)
+  p.n_chunks = (int32_t)attend_parts((kv->fmt == kMx4 && p.block_rows == 16 ? 3 : 2) * (int64_t)kv->n_cus, kv->fmt, blocks, len, per_seq);
   const int64_t tile = p.block_rows == 128 ? 64 : 32;
   p.piece_tiles = (int32_t)(((len + tile - 1) / tile + p.n_chunks - 1) / p.n_chunks);
   plan_space(p);
