@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64) void tdk_kv_append_rope_kernel(const KvDev kv, 
         }
         if (!same_b) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(y[i], u[i].x, c + 8 < R16 ? -(q[i] * u[i].y) : q[i] * u[i].y);
+          for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(y[i], u[i].x, q[i] * u[i].y);      // (a second member always: R16 < 8)
         }
       }
     }
