@@ -121,9 +121,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR && NR 
 }
 
 template <bool FOUR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_tile_kernel(const KvDev kv, const KvAttendDev at,
-                                                                                                            const int last_id) {
-  attend_steps<FOUR ? kMx4 : kBf16>(kv, at, last_id);
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tdk_kv_attend_tile_kernel(const KvDev kv, const KvAttendDev at) {
+  attend_steps<FOUR>(kv, at);
 }
 
 __global__ __launch_bounds__(256) void tdk_kv_attend_join_kernel(const KvDev kv, const KvAttendDev at, int64_t rows) { join_parts(kv, at, rows); }
@@ -158,7 +157,7 @@ hipError_t launch_kv_attend(const KvDev& kv, const KvAttendDev& at, const KvAtte
   if (fmt == kMx8) {
     e = launch_kv8_attend(kv, at, p, blocks, st);
   } else if (p.block_rows == 128) {
-    e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at, p.forward ? -1 : (int)(p.ids - 1));
+    e = launch(four ? tdk_kv_attend_tile_kernel<true> : tdk_kv_attend_tile_kernel<false>, blocks, 256, st, kv, at);
   } else {
     auto kernel = p.block_rows == 32 ? tdk_kv_attend_rows_kernel<true, 2> : four ? tdk_kv_attend_rows_kernel<true, 1> : tdk_kv_attend_rows_kernel<false, 1>;
     e = launch(kernel, blocks, 256, st, kv, at);

@@ -348,8 +348,7 @@ __device__ __forceinline__ void finish(const At& at, int64_t tok, int hq, int pi
 }
 
 // The same for a workgroup's part: finished if it is the only one, else kept for the join.
-template <class At>
-__device__ __forceinline__ void put_row(const At& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m, float l) {
+__device__ __forceinline__ void put_row(const KvAttendDev& at, int64_t tok, int hq, int chunk, int piece, const float (&o)[8], float m, float l) {
   if (at.n_chunks == 1) {
     finish(at, tok, hq, piece, o, m, l);
     return;
@@ -858,8 +857,8 @@ __device__ __forceinline__ void add_odd(const unsigned char* Vs, uint32_t live, 
   }
 }
 
-template <int FMT>
-__device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev at, const int last_id) {
+template <bool FOUR>
+__device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev at) {
   __shared__ __align__(16) StepShared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, hh = lane >> 5;
   int h;
@@ -869,7 +868,7 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
   // (several blocks per sequence: a causal prompt's last rows see most and start first; one: the numbers without a block come last, ahead of
   // the others they leave some compute units with one workgroup and others with three; 64 sequences of 4000 tokens, 20 rows: 274 -> 202 us)
   const int place = rest / at.n_chunks;
-  if (!find_block(kv, at, last_id < 0 ? place : last_id - place, kBlockRows, lane, b)) return;
+  if (!find_block(kv, at, at.last_id < 0 ? place : at.last_id - place, kBlockRows, lane, b)) return;
   h = (h + b.s + chunk) % kv.heads;
   const Tiles tiles = tiles_of(kv, at, b, kBigTile);
   int t_begin, t_end;
@@ -996,7 +995,7 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
     pages.start(kv, b.s, tiles, t_begin, 1, t_end, lane);
     int ok = there(pages.get(0));
     Codes ck[2], cv[2];                      // 4 bits: K of the step behind the next and V of the next one, and both of the step after
-    if constexpr (FMT != kBf16) {
+    if constexpr (FOUR) {
       const Codes k0 = fetch_codes(kv, kv.k, pages.get(0), h, wave, lane), k1 = fetch_codes(kv, kv.k, pages.get(1), h, wave, lane);
       Codes v0 = fetch_codes(kv, kv.v, pages.get(0), h, wave, lane);
       ck[0] = fetch_codes(kv, kv.k, pages.get(2), h, wave, lane);
@@ -1036,7 +1035,7 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
         __syncthreads();
       }
       const int ok_next = there(pages.get(1));
-      if constexpr (FMT != kBf16) {          // (nobody reads these two tiles in this step)
+      if constexpr (FOUR) {                  // (nobody reads these two tiles in this step)
         int ln = lane;
         asm volatile("" : "+v"(ln));
         put_codes<false>(ck[odd], sh.k[odd], wave, ln);
@@ -1053,7 +1052,7 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
       if (active) {
         float mx;
         int ln = lane;
-        if (FMT != kBf16) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
+        if (FOUR) asm volatile("" : "+v"(ln));         // (the places in the tiles are worked out again: kept from step to step they spill)
         // (past the last step: scores that are not used)
         if (far) {
           const float ref = reference(st.m_run);
@@ -1067,7 +1066,7 @@ __device__ __forceinline__ void attend_steps(const KvDev kv, const KvAttendDev a
           settle(mx);
         }
       }
-      if constexpr (FMT == kBf16) {
+      if constexpr (!FOUR) {
         landed();
         if (i + 1 < t_end) check_v(i + 1, ok, odd ^ 1);
       }
