@@ -83,7 +83,8 @@ typedef struct {
  *   TURNS    by the turns r_j = original_len f_j / (2 pi) that a pair makes: those below `low` are divided by factor, those above
  *            `high` stay, between them the share (r_j - low) / (high - low) of f_j stays and the rest is divided
  *   INDEX    by the pair's number: with d(r) = rotary_dim ln(original_len / (2 pi r)) / (2 ln theta), the number of the pair that makes r
- *            turns, the divided share grows from 0 at a = max(floor d(high), 0) to 1 at b = min(ceil d(low), rotary_dim - 1)
+ *            turns, the divided share grows from 0 at a = max(floor d(high), 0) to 1 at b = min(ceil d(low), rotary_dim - 1); where b is
+ *            not above a, the pairs up to a stay and those behind are divided
  * magnitude: cosines and sines are multiplied by it (in double, before they are rounded to fp32).  Fields that a scaling does not use are
  * not looked at.  Errors of the calls that take one: UNSUPPORTED (rotary_dim not a multiple of 16 from 16 to 128, unknown scaling),
  * INVALID_ARG (magnitude outside [1e-6, 1e6], factor below 1, original_len not positive, not 0 < low < high; INDEX with theta <= 1). */
@@ -392,7 +393,8 @@ tdk_status tdk_restore_layers(tdk_round* r, int32_t first_layer, int32_t n_layer
  *   TDK_KV_BF16    planes [pool_pages][T][H][D] bf16: the pool of the rounds (tdk_layer_io.pool_k / pool_v)
  *   TDK_KV_MXFP8   planes [pool_pages][H][T * 128 + T * 4] bytes, 1.94 times smaller: as MXFP4, but a value is a byte: one sign, four
  *                  exponent bits (bias 7) and three mantissa bits, magnitudes up to 448; 0x7f and 0xff are NaN.  A block's byte
- *                  255 makes all 32 NaN; values are infinite from 2^128 on (bytes from 247).
+ *                  255 makes all 32 NaN; values are infinite from 2^128 on (bytes from 247), and below 2^-124 (bytes 0 to 2, which append
+ *                  does not write) they are rounded to bf16's grid of 2^-133.
  *   TDK_KV_MXFP4   planes [pool_pages][H][T * 64 + T * 4] bytes, 3.8 times smaller: per page and KV head the 4-bit
  *                  values of its T tokens (64 bytes each, element 2 i in the low half of byte i), then the
  *                  block exponents (4 bytes each).  A value is one sign, two exponent bits and one mantissa bit
@@ -506,7 +508,7 @@ tdk_status tdk_kv_read(const tdk_kv* kv, const tdk_kv_cache* cache, const tdk_kv
  * Any scale up to 2^127 in magnitude is taken, zero and denormal ones as they are (scores q . K beyond fp32 are infinite
  * before they are scaled; a query all of whose scores are minus infinity counts as one that sees nothing).  What a query
  * does not see does not reach its result, whatever it holds (NaN and infinities included).  What it does see does: a NaN in V makes its element
- * NaN, an infinity makes it infinite, or NaN where the weight is below fp32's range.  bf16 products with fp32 sums;
+ * NaN, an infinity makes it infinite, or NaN where it meets the other one or its weight is below fp32's range.  bf16 products with fp32 sums;
  * the softmax weights are rounded to bf16 for the second product, their sum is not.  Allocates nothing, one or two
  * kernels, does not synchronise; results do not depend on what else runs. */
 typedef struct {
@@ -551,7 +553,8 @@ typedef struct {
 
 /* As tdk_kv_attend_io, with rows k and v of [H][D] bf16 (strides at most 2^24 elements).  out_f32: out is fp32 (out_stride in elements of
  * it), so that it can be another call's part_out: a prompt attends to its own rows here and to its history in the pages with
- * tdk_kv_attend, whose hole is the prompt's span. */
+ * tdk_kv_attend, whose hole is the prompt's span.  It saves the rounding of the result, not that of the weights to bf16, which is in it as in every
+ * result of these calls: 2^-8 of the weighted sum of |V| at most. */
 typedef struct {
   const void*    q;
   int64_t        q_stride;

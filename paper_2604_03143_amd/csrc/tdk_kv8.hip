@@ -130,7 +130,8 @@ struct PageSource {
 
 }  // namespace
 
-// Read: bounded by memory: 20 851 tokens (8 heads) 27 us, 4.8 TB/s of codes read and bf16 written; 250 tokens 2.9.
+// Read: 20 851 tokens (8 heads) 27 us, 4.8 TB/s of codes read and bf16 written; 250 tokens 2.9.  What bounds it is the order of a wavefront's reads, not yet memory (a copy has
+// 6.7): the sequence is searched twice, one search behind the other (read_rows, slot_of), and a step's codes are asked for when those before are written.
 template <bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv8_read_kernel(const KvDev kv, const KvRowsDev rows) {
   read_rows<kMx8, ONCE>(kv, rows);
@@ -146,8 +147,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   attend_rows<kMx8, NR>(kv, at);
 }
 
-// More rows: attend_in_steps.  Prompts of up to 2048 tokens behind 4000, 5 queries a head: 469 us, 890 TFLOP/s; four whole ones 949 (a prompt whose rows need no
-// conversion: 1121).  Bounded by vector instructions, a fifth of which bring the pages (46 % busy, matrix cores 39 %), and by unequal blocks in three rounds of
+// More rows: attend_in_steps.  Prompts of up to 2048 tokens behind 4000, 5 queries a head: 469 to 496 us by card, 842 to 890 TFLOP/s; four whole ones 949 (a prompt whose
+// rows need no conversion: 1043 to 1121).  Bounded by vector instructions, a fifth of which bring the pages (46 % busy, matrix cores 39 %), and by unequal blocks in three rounds of
 // workgroups.  Fewer instructions there made it faster: a wavefront asks for its own page alone (507 -> 493 us), works out a lane's four places in a tile from
 // one (-> 484), sees by codes and powers whether V is finite (492 -> 481 on another card); an order of the writes without bank conflicts (10 % of LDS's time) costs more than it saves.  The body without the pipeline that paged
 // bf16 has took 669 us for 515 at the time.  40 rows over 64 sequences of 4000 tokens: 118 us.

@@ -101,7 +101,8 @@ __global__ __launch_bounds__(MANY ? 256 : 64) void tdk_kv_rotate_kernel(const Kv
 // Append, the forms that tdk_kv_append_kernel does not have: lanes and steps as there.  A piece whose pair lies in another lane (half layout, part of the
 // head) gets its partner by exchanges: piece k < R / 8 pairs with the one R / 16 further on, or back.
 // What bounds it: writes that lie scattered.  20 851 tokens into 8-bit pages (8 + 64 heads): 143 us, 5.7 TB/s; 250 tokens 5.1 us.  One wavefront per token: with four,
-// as the rotation has them, the call took 183 us instead of 172 together with the read behind it.
+// as the rotation has them, the call took 183 us instead of 172 together with the read behind it.  Half of the head, or a magnitude, 20 000 tokens of 8 + 40 heads: into bf16
+// pages 103 us, 5.55 TB/s (plain rotation, four wavefronts per token: 100 us, 5.7), into 4 bits 92 to 95, 5.4 to 5.6 (plain 97); 12 500 tokens 68 (65) and 62 to 64 (65).
 // ---------------------------------------------------------------------------------------------
 template <int FMT, bool ONCE>
 __global__ __launch_bounds__(64) void tdk_kv_append_rope_kernel(const KvDev kv, const KvRowsDev rows) {

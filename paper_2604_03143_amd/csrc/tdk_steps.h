@@ -111,8 +111,8 @@ __device__ __forceinline__ void step_of_rows(const unsigned char* Ks, const unsi
 
 // A row's weights are 2^(c (s - m) - 12), s its scores, c the scale times log2 e, m a reference point that follows their maximum only from 2^11.5 on, so that
 // sums and products (both fp32) are seldom scaled again; weights go to the second products as bf16 (half a step of 2^-8 each, the error that is left).
-// What bounds it: the clock that matrix and vector units share under load.  A prompt of 8192 tokens, 8 heads with 5 queries each: 613 us, 1121 TFLOP/s of what the
-// queries see where a matrix product of 16 384 reaches 1364; counters: matrix cores 65 % busy, vector units 55 %, 1.7 GHz, no bank conflicts.
+// What bounds it: the clock that matrix and vector units share under load.  A prompt of 8192 tokens, 8 heads with 5 queries each: 613 to 659 us by card, 1043 to 1121
+// TFLOP/s of what the queries see where a matrix product of 16 384 reaches 1364; counters: matrix cores 65 % busy, vector units 55 %, 1.7 GHz, no bank conflicts.
 // Why so: two workgroups of four wavefronts on a compute unit, 32 rows a wavefront.  64 rows a wavefront spill (1175 us for 720 at the time), eight
 // wavefronts a workgroup wait for one another (676 for 660, 25 short prompts 158 for 138).  Steps that every row sees whole skip all tests by
 // one scalar; the maxima of the next scores stand in the slots of the second products (719 -> 663 us with scalar borders, 655 with that scalar).
